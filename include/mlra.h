@@ -243,6 +243,69 @@ MLRA_API int mlra_pre_attention(const mlra_cache* cache, const mlra_pre_weights*
                        const void* hidden, const int32_t* positions, void* q_nope, void* q_rope,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* Latent cache in 4 bits (OCP microscaling, E2M1 elements with E8M0 scales).  32 neighbouring channels of one token
+ * and block share a power of two and each channel is a 4-bit code, so that a token of MLRA-4 (512 latent and 64 RoPE
+ * channels) takes 400 bytes instead of 1152.  The RoPE key keeps the type `dtype`, which is also that of queries,
+ * weights and gate.
+ *   code c = sign << 3 | e << 1 | m stands for (-1)^sign {0, 0.5, 1, 1.5, 2, 3, 4, 6}[c & 7] 2^(E - 127) with the scale
+ *   byte E of its group; E = 255: every channel of the group is NaN.
+ * d_cb must be a multiple of 32; `latent` and `rope` are 16-byte aligned (MLRA_ERR_SHAPE otherwise). */
+typedef struct mlra_mx4_cache {
+  void* latent;              /* device [num_pages][n_blocks][page_size][d_cb/2]: channel 2i in the low half of byte i */
+  void* scales;              /* device [num_pages][n_blocks][page_size][d_cb/32] bytes E                              */
+  void* rope;                /* device [num_pages][page_size][d_r] of dtype                                           */
+  const int32_t* page_table; /* device [batch][max_pages_per_seq]                                                     */
+  const int32_t* seq_lens;   /* device [batch]; read by mlra_mx4_decode_attn only, and may be NULL elsewhere          */
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t max_pages_per_seq;
+  int32_t n_blocks;
+  int32_t d_cb;
+  int32_t d_r;
+  int32_t dtype;             /* mlra_dtype */
+} mlra_mx4_cache;
+
+/* Quantises rows as it writes them (as mlra_append_kv, for one token or a piece of a prompt): row j of sequence s goes to
+ * slot positions[s] + j, j < n = min(row_lens[s], n_rows).
+ *   c_kv [batch][n_rows][n_blocks*d_cb], k_rope [batch][n_rows][d_r] of src_dtype (RoPE keys are rounded to dtype)
+ *   positions [batch] int32: first slot; < 0 skips the sequence
+ *   row_lens  [batch] int32, or NULL: n_rows rows each
+ * E = clamp(x - 2 + 127, 2, 252) with x the exponent of the group's largest magnitude as one mantissa bit rounds it (1.75 2^e
+ * counts as 2^(e+1)); codes are the channels divided by 2^(E - 127), rounded to nearest, ties to the even m, cut off at 6.  A
+ * group with an infinity or a NaN becomes E = 255.  Rows whose slot lies beyond the capacity max_pages_per_seq * page_size or
+ * whose page id is not in [0, num_pages) are skipped.  Pages that two sequences write must not be the same. */
+MLRA_API int mlra_mx4_append_kv(const mlra_mx4_cache* cache, int32_t batch, int32_t n_rows, const void* c_kv,
+                       const void* k_rope, int32_t src_dtype, const int32_t* positions, const int32_t* row_lens,
+                       void* stream);
+
+/* The inverse: slots positions[s] + j, j < min(row_lens[s], n_rows), of every sequence as the values that they stand for.
+ *   c_kv_out [batch][n_rows][n_blocks*d_cb], k_rope_out [batch][n_rows][d_r] of dst_dtype (latents are exact in either type,
+ *   fp32 RoPE keys are rounded to bf16)
+ * Rows that mlra_mx4_append_kv would skip, and rows from row_lens[s] on, are left as they were. */
+MLRA_API int mlra_mx4_read_kv(const mlra_mx4_cache* cache, int32_t batch, int32_t n_rows, const int32_t* positions,
+                     const int32_t* row_lens, void* c_kv_out, void* k_rope_out, int32_t dst_dtype, void* stream);
+
+/* Bytes of workspace for mlra_mx4_decode_attn on the current device (0 on invalid sizes); h is the total number of heads. */
+MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, int32_t groups, int32_t n_blocks,
+                                       int32_t d_cb, int32_t page_size, int32_t max_pages_per_seq);
+
+/* Decode attention on a cache in 4 bits: mlra_decode_attn_multi (groups = 1; n_blocks = 1 is MLA) and mlra2_decode_attn
+ * (groups = 2: h and n_blocks even, block b serves the h/2 heads of group b / (n_blocks/2)) in one call, with q_len >= 1 query
+ * tokens per sequence, query j of which sits at row seq_lens[s] - q_len + j and attends to the rows up to its own.  With
+ * hb = h / groups heads per block:
+ *   q_abs [batch][q_len][n_blocks][hb][d_cb], q_rope [batch][q_len][h][d_r], w_uv [n_blocks][d_cb][hb*d_h]: type dtype
+ *   gate  optional [batch][q_len][h][d_h] of dtype (as in mlra_decode_attn_gated)
+ *   out   [batch][q_len][h][d_h] of out_dtype; lse optional [batch][q_len][n_blocks][hb] fp32
+ *   softmax_scale: tau > 0, or MLRA_SCALE_FOLDED for queries from mlra_absorb_q_folded / mlra2_absorb_q_folded
+ * The arithmetic is that of a cache of type dtype that holds the same values: bf16 rounds the probabilities and the merged
+ * values to bf16, fp32 rounds nothing to fewer than 24 bits.  A query without a row gives zeros and lse = -inf.  d_cb <= 512,
+ * d_r <= 128; pages, lengths and page ids as for mlra_decode_attn (lengths beyond the capacity count as the capacity).
+ * Deterministic. */
+MLRA_API int mlra_mx4_decode_attn(const mlra_mx4_cache* cache, int32_t batch, int32_t q_len, int32_t h, int32_t d_h,
+                         int32_t groups, const void* q_abs, const void* q_rope, const void* w_uv, const void* gate,
+                         float softmax_scale, float out_scale, void* out, int32_t out_dtype, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
 /* Workspace bytes for gqa_decode_attn (0 on invalid sizes). */
 MLRA_API size_t gqa_decode_workspace_bytes(int32_t batch, int32_t h, int32_t d_h, int32_t max_seq_len);
 

@@ -24,12 +24,21 @@ EXPORTS = ("mlra_strerror", "mlra_append_kv", "mlra_absorb_q", "mlra_absorb_q_fo
            "mlra_decode_attn", "mlra_decode_attn_static", "mla_decode_attn", "mlra2_absorb_q", "mlra2_decode_workspace_bytes",
            "mlra2_decode_attn", "mlra_decode_attn_gated", "mlra_decode_multi_workspace_bytes", "mlra_decode_attn_multi",
            "mlra_pre_attention_workspace_bytes", "mlra_pre_attention",
+           "mlra_mx4_append_kv", "mlra_mx4_read_kv", "mlra_mx4_decode_workspace_bytes", "mlra_mx4_decode_attn",
            "gqa_decode_workspace_bytes", "gqa_decode_attn", "mlra_kernel_timing_begin",
            "mlra_kernel_timing_end", "mlra_decode_plan_info", "mlra_decode_route_info", "mlra_probe_stream_read", "mlra_probe_shader_clock")
 
 
 class _CacheStruct(ctypes.Structure):
     _fields_ = [("latent", ctypes.c_void_p), ("rope", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages_per_seq", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
+                ("d_cb", ctypes.c_int32), ("d_r", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _Mx4CacheStruct(ctypes.Structure):
+    _fields_ = [("latent", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rope", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
                 ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("max_pages_per_seq", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
@@ -91,6 +100,15 @@ def load_library() -> ctypes.CDLL:
     lib.mlra_pre_attention_workspace_bytes.argtypes = [i32] * 9
     lib.mlra_pre_attention.restype = ctypes.c_int
     lib.mlra_pre_attention.argtypes = [cp, ctypes.POINTER(_PreWeightsStruct), i32, vp, vp, vp, vp, vp, sz, vp]
+    mp = ctypes.POINTER(_Mx4CacheStruct)
+    lib.mlra_mx4_append_kv.restype = ctypes.c_int
+    lib.mlra_mx4_append_kv.argtypes = [mp, i32, i32, vp, vp, i32, vp, vp, vp]
+    lib.mlra_mx4_read_kv.restype = ctypes.c_int
+    lib.mlra_mx4_read_kv.argtypes = [mp, i32, i32, vp, vp, vp, vp, i32, vp]
+    lib.mlra_mx4_decode_workspace_bytes.restype = sz
+    lib.mlra_mx4_decode_workspace_bytes.argtypes = [i32] * 8
+    lib.mlra_mx4_decode_attn.restype = ctypes.c_int
+    lib.mlra_mx4_decode_attn.argtypes = [mp, i32, i32, i32, i32, i32, vp, vp, vp, vp, f32, f32, vp, i32, vp, vp, sz, vp]
     lib.mla_decode_attn.restype = ctypes.c_int
     lib.mla_decode_attn.argtypes = [cp, i32, i32, i32, vp, vp, vp, f32, vp, i32, vp, vp, sz, vp]
     lib.mlra_decode_plan_info.restype = ctypes.c_int
@@ -441,6 +459,110 @@ def mlra_pre_attention(cache: Cache, weights: PreWeights, hidden: torch.Tensor, 
                                   workspace.numel() * workspace.element_size(), _stream(stream)),
            "mlra_pre_attention")
     return q_nope, q_rope
+
+
+@dataclass
+class Mx4Cache:
+    """Paged latent KV cache in 4 bits (struct mlra_mx4_cache): device tensors plus their dimensions."""
+
+    latent: torch.Tensor      # [num_pages][n_blocks][page_size][d_cb / 2] uint8, two codes a byte
+    scales: torch.Tensor      # [num_pages][n_blocks][page_size][d_cb / 32] uint8
+    rope: torch.Tensor        # [num_pages][page_size][d_r] bfloat16 or float32
+    page_table: torch.Tensor  # [batch][max_pages_per_seq] int32
+    seq_lens: torch.Tensor    # [batch] int32
+
+    @classmethod
+    def empty(cls, num_pages: int, n_blocks: int, page_size: int, d_cb: int, d_r: int, page_table: torch.Tensor,
+              seq_lens: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> "Mx4Cache":
+        """Pools without contents, on page_table's device."""
+        assert d_cb % 32 == 0
+        dev = page_table.device
+        pool = lambda width, t: torch.empty((num_pages, n_blocks, page_size, width), dtype=t, device=dev)
+        return cls(pool(d_cb // 2, torch.uint8), pool(d_cb // 32, torch.uint8),
+                   torch.empty((num_pages, page_size, d_r), dtype=dtype, device=dev), page_table, seq_lens)
+
+    def struct(self) -> _Mx4CacheStruct:
+        P, NB, ps, half = self.latent.shape
+        assert self.latent.dtype == torch.uint8 and self.scales.dtype == torch.uint8
+        assert self.scales.shape == (P, NB, ps, half // 16) and half % 16 == 0
+        assert self.rope.shape[:2] == (P, ps) and self.rope.dim() == 3
+        assert self.page_table.dtype == torch.int32 and self.seq_lens.dtype == torch.int32
+        return _Mx4CacheStruct(_ptr(self.latent), _ptr(self.scales), _ptr(self.rope), _ptr(self.page_table),
+                               _ptr(self.seq_lens), P, ps, self.page_table.shape[1], NB, 2 * half, self.rope.shape[2],
+                               _dt(self.rope.dtype))
+
+    @property
+    def max_seq_len(self) -> int:
+        return int(self.page_table.shape[1] * self.latent.shape[2])
+
+
+def _mx4_rows(cs: _Mx4CacheStruct, c_kv, k_rope, positions, row_lens):
+    batch, n_rows, d_c = c_kv.shape
+    assert d_c == cs.n_blocks * cs.d_cb and k_rope.shape == (batch, n_rows, cs.d_r) and c_kv.dtype == k_rope.dtype
+    for t in (positions, row_lens):
+        assert t is None or (t.dtype == torch.int32 and t.shape == (batch,))
+    return batch, n_rows
+
+
+def mlra_mx4_append_kv(cache: Mx4Cache, c_kv: torch.Tensor, k_rope: torch.Tensor, positions: torch.Tensor,
+                       new_lens: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Quantises rows c_kv [batch][n_rows][n_blocks*d_cb], k_rope [batch][n_rows][d_r] into slots positions[s] + j,
+    j < new_lens[s] (n_rows if not given)."""
+    cs = cache.struct()
+    batch, n_rows = _mx4_rows(cs, c_kv, k_rope, positions, new_lens)
+    assert cache.page_table.shape[0] == batch
+    _check(load_library().mlra_mx4_append_kv(ctypes.byref(cs), batch, n_rows, _ptr(c_kv), _ptr(k_rope), _dt(c_kv.dtype),
+                                             _ptr(positions), _ptr(new_lens), _stream(stream)), "mlra_mx4_append_kv")
+
+
+def mlra_mx4_read_kv(cache: Mx4Cache, positions: torch.Tensor, row_lens: Optional[torch.Tensor], c_kv_out: torch.Tensor,
+                     k_rope_out: torch.Tensor, stream=None):
+    """Slots positions[s] + j, j < row_lens[s] (all rows of the outputs if None), into row j of c_kv_out
+    [batch][n_rows][n_blocks*d_cb] and k_rope_out [batch][n_rows][d_r]; the rows behind them are left as they were."""
+    cs = cache.struct()
+    batch, n_rows = _mx4_rows(cs, c_kv_out, k_rope_out, positions, row_lens)
+    assert cache.page_table.shape[0] == batch
+    _check(load_library().mlra_mx4_read_kv(ctypes.byref(cs), batch, n_rows, _ptr(positions), _ptr(row_lens), _ptr(c_kv_out),
+                                           _ptr(k_rope_out), _dt(c_kv_out.dtype), _stream(stream)), "mlra_mx4_read_kv")
+    return c_kv_out, k_rope_out
+
+
+def mlra_mx4_decode_workspace_bytes(batch: int, q_len: int, h: int, groups: int, n_blocks: int, d_cb: int, page_size: int,
+                                    max_pages_per_seq: int) -> int:
+    return int(load_library().mlra_mx4_decode_workspace_bytes(batch, q_len, h, groups, n_blocks, d_cb, page_size,
+                                                              max_pages_per_seq))
+
+
+def mlra_mx4_decode_attn(cache: Mx4Cache, q_abs: torch.Tensor, q_rope: torch.Tensor, w_uv: torch.Tensor, softmax_scale: float,
+                         out_scale: float = 1.0, groups: int = 1, gate: Optional[torch.Tensor] = None,
+                         out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                         lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """q_abs [batch][q_len][n_blocks][h / groups][d_cb], q_rope [batch][q_len][h][d_r] -> out [batch][q_len][h][d_h]; without
+    the q_len dimension (one query token) in all of them, out has none either."""
+    cs = cache.struct()
+    single = q_abs.dim() == 4
+    lead = tuple(q_abs.shape[:1]) if single else tuple(q_abs.shape[:2])
+    n_blocks, hb, d_cb = q_abs.shape[-3:]
+    batch, q_len, h, d_h = lead[0], 1 if single else lead[1], hb * groups, w_uv.shape[2] // hb
+    assert (n_blocks, d_cb) == (cs.n_blocks, cs.d_cb) and w_uv.shape == (n_blocks, d_cb, hb * d_h)
+    assert q_rope.shape == lead + (h, cs.d_r) and cache.page_table.shape[0] == batch and cache.seq_lens.shape == (batch,)
+    for t in (q_abs, q_rope, w_uv) + (() if gate is None else (gate,)):
+        assert t.dtype == cache.rope.dtype
+    assert gate is None or gate.shape == lead + (h, d_h)
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == lead + (n_blocks, hb))
+    if out is None:
+        out = torch.empty(lead + (h, d_h), dtype=out_dtype or q_abs.dtype, device=q_abs.device)
+    assert out.shape == lead + (h, d_h)
+    if workspace is None:
+        need = mlra_mx4_decode_workspace_bytes(batch, q_len, h, groups, n_blocks, d_cb, cs.page_size, cs.max_pages_per_seq)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q_abs.device)
+    _check(load_library().mlra_mx4_decode_attn(ctypes.byref(cs), batch, q_len, h, d_h, groups, _ptr(q_abs), _ptr(q_rope),
+                                               _ptr(w_uv), _ptr(gate), float(softmax_scale), float(out_scale), _ptr(out),
+                                               _dt(out.dtype), _ptr(lse), _ptr(workspace),
+                                               workspace.numel() * workspace.element_size(), _stream(stream)),
+           "mlra_mx4_decode_attn")
+    return out
 
 
 def gqa_decode_workspace_bytes(batch: int, h: int, d_h: int, max_seq_len: int) -> int:

@@ -253,11 +253,135 @@ static int decode_common(const mlra_cache* c, int batch, int h, int groups, int 
   return st;
 }
 
+// ---- latent cache in 4 bits ---------------------------------------------------------------------------------------
+static int check_mx4_cache(const mlra_mx4_cache* c, int batch) {
+  if (!valid_dtype(c->dtype)) return MLRA_ERR_DTYPE;
+  if (batch <= 0 || batch > 65535 || c->n_blocks <= 0 || c->d_cb <= 0 || c->d_cb % 32 != 0 || c->d_r <= 0 || c->page_size <= 0 ||
+      c->max_pages_per_seq <= 0 || c->num_pages <= 0)
+    return MLRA_ERR_SHAPE;
+  if ((long)c->n_blocks * c->d_cb > 8192 || (long)c->max_pages_per_seq * c->page_size > 0x7fffffffL) return MLRA_ERR_SHAPE;
+  if (((uintptr_t)c->latent | (uintptr_t)c->rope) % 16 != 0) return MLRA_ERR_SHAPE;
+  return MLRA_OK;
+}
+
+static int mx4_rows_common(const mlra_mx4_cache* c, int batch, int n_rows, const void* c_kv, const void* k_rope, int dtype,
+                           const int32_t* positions) {
+  if (!c || !c_kv || !k_rope || !positions) return MLRA_ERR_NULL;
+  if (!c->latent || !c->scales || !c->rope || !c->page_table) return MLRA_ERR_NULL;
+  if (!valid_dtype(dtype)) return MLRA_ERR_DTYPE;
+  if (n_rows <= 0 || n_rows > (1 << 26)) return MLRA_ERR_SHAPE;
+  return check_mx4_cache(c, batch);
+}
+
+// Two rounds of the decode kernel's workgroups run at a time on a compute unit.
+static SplitPlan plan_mx4(int units, int h, int n_blocks, int d_cb, int max_seq_len, int cus) {
+  return plan_splits(units, n_blocks * ((h + 63) / 64), max_seq_len, 2 * cus);
+}
+
+// (q_len > 1: a row of the lengths and of the page table per query in front of the partials)
+static size_t mx4_table_bytes(int units, int q_len, int max_pages) {
+  return q_len == 1 ? 0 : align_up((size_t)units * sizeof(int32_t), 256) +
+                              align_up((size_t)units * max_pages * sizeof(int32_t), 256);
+}
+
+static bool mx4_shape_ok(int batch, int q_len, int h, int groups, int n_blocks, int d_cb, int page_size, int max_pages) {
+  return batch > 0 && q_len > 0 && h > 0 && h <= 65535 && (groups == 1 || groups == 2) && n_blocks > 0 && d_cb > 0 &&
+         d_cb % 32 == 0 && d_cb <= kMx4MaxBlock && (long)n_blocks * d_cb <= 8192 && page_size > 0 && max_pages > 0 &&
+         (long)batch * q_len <= 65535 && h % groups == 0 && n_blocks % groups == 0 &&
+         (long)max_pages * page_size <= 0x7fffffffL;
+}
+
 }  // namespace mlra
 
 using namespace mlra;
 
 extern "C" {
+
+int mlra_mx4_append_kv(const mlra_mx4_cache* c, int32_t batch, int32_t n_rows, const void* c_kv, const void* k_rope,
+                       int32_t src_dtype, const int32_t* positions, const int32_t* row_lens, void* stream) {
+  const int st = mx4_rows_common(c, batch, n_rows, c_kv, k_rope, src_dtype, positions);
+  if (st != MLRA_OK) return st;
+  return launch_mx4_append(c, batch, n_rows, c_kv, k_rope, src_dtype, positions, row_lens, (hipStream_t)stream);
+}
+
+int mlra_mx4_read_kv(const mlra_mx4_cache* c, int32_t batch, int32_t n_rows, const int32_t* positions,
+                     const int32_t* row_lens, void* c_kv_out, void* k_rope_out, int32_t dst_dtype, void* stream) {
+  const int st = mx4_rows_common(c, batch, n_rows, c_kv_out, k_rope_out, dst_dtype, positions);
+  if (st != MLRA_OK) return st;
+  return launch_mx4_read(c, batch, n_rows, positions, row_lens, c_kv_out, k_rope_out, dst_dtype, (hipStream_t)stream);
+}
+
+size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, int32_t groups, int32_t n_blocks,
+                                       int32_t d_cb, int32_t page_size, int32_t max_pages_per_seq) {
+  if (!mx4_shape_ok(batch, q_len, h, groups, n_blocks, d_cb, page_size, max_pages_per_seq)) return 0;
+  const int units = batch * q_len, hb = h / groups;
+  return mx4_table_bytes(units, q_len, max_pages_per_seq) +
+         decode_ws_bytes(units, hb, n_blocks, d_cb,
+                         plan_mx4(units, hb, n_blocks, d_cb, max_pages_per_seq * page_size, device_cu_count()));
+}
+
+int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, int32_t h, int32_t d_h, int32_t groups,
+                         const void* q_abs, const void* q_rope, const void* w_uv, const void* gate, float softmax_scale,
+                         float out_scale, void* out, int32_t out_dtype, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  if (!c || !q_abs || !q_rope || !w_uv || !out) return MLRA_ERR_NULL;
+  if (!c->latent || !c->scales || !c->rope || !c->page_table || !c->seq_lens) return MLRA_ERR_NULL;
+  if (!valid_dtype(out_dtype)) return MLRA_ERR_DTYPE;
+  const int bad = check_mx4_cache(c, batch);
+  if (bad != MLRA_OK) return bad;
+  if (d_h <= 0 || c->d_r > kMx4MaxRope ||
+      !mx4_shape_ok(batch, q_len, h, groups, c->n_blocks, c->d_cb, c->page_size, c->max_pages_per_seq))
+    return MLRA_ERR_SHAPE;
+  const int units = batch * q_len, hb = h / groups, max_seq_len = c->max_pages_per_seq * c->page_size;
+  const size_t need = mlra_mx4_decode_workspace_bytes(batch, q_len, h, groups, c->n_blocks, c->d_cb, c->page_size,
+                                                      c->max_pages_per_seq);
+  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 256 != 0) return MLRA_ERR_WORKSPACE;
+  DecodeArgs a = {};
+  a.cus = device_cu_count();
+  a.plan = plan_mx4(units, hb, c->n_blocks, c->d_cb, max_seq_len, a.cus);
+  a.latent = c->latent;
+  a.scales = c->scales;
+  a.rope = c->rope;
+  a.page_table = c->page_table;
+  a.seq_lens = c->seq_lens;
+  a.page_size = c->page_size;
+  a.max_pages = c->max_pages_per_seq;
+  a.n_blocks = c->n_blocks;
+  a.d_cb = c->d_cb;
+  a.d_r = c->d_r;
+  a.batch = units;
+  a.h = hb;
+  a.d_h = d_h;
+  a.groups = groups;
+  a.q_abs = q_abs;
+  a.q_rope = q_rope;
+  a.w_uv = w_uv;
+  a.softmax_scale = softmax_scale;
+  a.out_scale = out_scale;
+  a.out = out;
+  a.out_dtype = out_dtype;
+  a.lse = lse;
+  a.gate = gate;
+  a.q_group = q_len;
+  a.dtype = c->dtype;
+  a.stream = (hipStream_t)stream;
+  char* ws = (char*)workspace;
+  if (q_len > 1) {
+    int32_t* const lens = (int32_t*)ws;
+    int32_t* const table = (int32_t*)(ws + align_up((size_t)units * sizeof(int32_t), 256));
+    const int st = launch_expand_queries(c->seq_lens, c->page_table, batch, q_len, c->max_pages_per_seq, lens, table, a.stream);
+    if (st != MLRA_OK) return st;
+    a.seq_lens = lens;
+    a.page_table = table;
+    ws += mx4_table_bytes(units, q_len, c->max_pages_per_seq);
+  }
+  const size_t parts = (size_t)units * c->n_blocks * a.plan.n_splits * hb;
+  a.part_z = (float*)ws;
+  a.part_ml = (float*)(ws + align_up(parts * c->d_cb * sizeof(float), 256));
+  const int st = launch_mx4_decode(a);
+  if (st != MLRA_OK) return st;
+  return merge_upproj_mfma_supported(a) ? launch_merge_upproj_mfma(a) : launch_merge_upproj_f32(a);
+}
 
 const char* mlra_strerror(int status) {
   switch (status) {

@@ -116,6 +116,7 @@ struct DecodeArgs {
   int dtype;
   hipStream_t stream;
   KernelTimer t_main, t_epi;   // set by mlra_kernel_timing_begin: the decode kernel and the merge / up-projection
+  const void* scales = nullptr;   // of a latent cache in 4 bits ([num_pages][n_blocks][page_size][d_cb / 32]); null: none
 };
 
 // Factor that takes the raw score to the log2 domain: tau log2(e), or 1 when the caller's queries already
@@ -180,6 +181,15 @@ bool gqa_mfma_supported(const GqaArgs& a);
 int launch_gqa_mfma(const GqaArgs& a);
 bool gqa_mfma_writes_output(const GqaArgs& a);   // nothing is left for launch_gqa_merge
 int launch_gqa_merge(const GqaArgs& a);
+
+// ---- latent cache in 4 bits ----------------------------------------------------------------------
+int launch_mx4_append(const mlra_mx4_cache* c, int batch, int n_rows, const void* c_kv, const void* k_rope, int src_dtype,
+                      const int32_t* positions, const int32_t* row_lens, hipStream_t stream);
+int launch_mx4_read(const mlra_mx4_cache* c, int batch, int n_rows, const int32_t* positions, const int32_t* row_lens,
+                    void* c_kv, void* k_rope, int dst_dtype, hipStream_t stream);
+constexpr int kMx4MaxBlock = 512, kMx4MaxRope = 128;   // channels that the decode kernel takes
+int mx4_heads_per_wg(int h, int d_cb, int dtype);
+int launch_mx4_decode(const DecodeArgs& a);
 
 // ---- pre-attention of the new token (pre_attn.hip) ----------------------------------------------
 // Weight matrices that share their rows (the K dimension) and sit side by side in the output.

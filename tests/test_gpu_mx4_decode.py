@@ -1,0 +1,168 @@
+"""Decode attention on a 4-bit latent cache against the fp64 oracle.
+
+The cached values are exact, what is rounded is what a cache of the calls' type rounds, and the bars are those of its tests:
+1e-2 (bf16) and 1e-5 (fp32) of the largest output.  bf16: the queries (with the softmax scale), the probabilities, a chunk's
+row and the merged values are rounded by up to 2^-8 each; these errors are independent, 2^-8 / sqrt(3) in the mean, and sum up
+over the same products as the values do, so that four of them give 4.5e-3 of the root mean square output and five times that,
+2.3e-2, is less than 1e-2 of the largest one, which is three to four times as large.  fp32: sums of up to 10^4 terms of 2^-24."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as orc
+from paper_2603_02188_amd import binding as mlra
+
+from gpu_util import max_rel_err
+from mx4_util import DT, HostCache, queries, stored
+
+pytestmark = pytest.mark.gpu
+
+BAR = {"bf16": 1e-2, "f32": 1e-5}
+
+
+def _check(lens, n_blocks=4, d_cb=128, d_r=64, h=128, d_h=128, groups=1, q_len=1, page=64, dtype="bf16", out="f32", gated=False,
+           out_scale=1.0, max_pages=None, seed=1, single=False):
+    print(f"[case] lens={lens} nb={n_blocks} d_cb={d_cb} d_r={d_r} h={h} g={groups} q={q_len} page={page} {dtype}", flush=True)
+    hc = HostCache(lens, n_blocks, d_cb, d_r, dtype, page, seed, max_pages)
+    rng = np.random.default_rng([seed, 9])
+    batch, hb, tau = len(lens), h // groups, 1.0 / np.sqrt(d_h + d_r)
+    (qa, qa64), (qr, qr64), (wv, wv64) = queries(rng, batch, q_len, n_blocks, hb, groups, d_cb, d_r, d_h, dtype)
+    gate, gate64 = stored(1.0 / (1.0 + np.exp(-rng.standard_normal((batch, q_len, h, d_h)))), dtype) if gated else (None, None)
+    lse = torch.full((batch, q_len, n_blocks, hb), float("nan"), device="cuda")
+    squeeze = (lambda t: None if t is None else t[:, 0]) if single else (lambda t: t)
+    args = (hc.device(), squeeze(qa), squeeze(qr), wv, tau, out_scale)
+    kw = dict(groups=groups, gate=squeeze(gate), out_dtype=DT[out])
+    got = mlra.mlra_mx4_decode_attn(*args, lse=squeeze(lse), **kw)
+    again = mlra.mlra_mx4_decode_attn(*args, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(got, again)                                # deterministic, and the same without lse
+    ref, ref_lse = orc.attend(hc.rows, hc.ropes, lens, qa64, qr64, wv64, tau, out_scale, groups, gate64)
+    got = got.double().cpu().numpy().reshape(ref.shape)
+    err = max_rel_err(got, ref)
+    print(f"       max rel err {err:.3e} (bar {BAR[dtype]:g})", flush=True)
+    assert err <= BAR[dtype] + (2.0 ** -8 if out == "bf16" else 0.0)
+    lse = lse.double().cpu().numpy()
+    empty = np.isneginf(ref_lse)
+    assert np.isneginf(lse[empty]).all()
+    if not empty.all():
+        # bf16: rounded queries move a score by 2^-8 of its terms' root sum of squares, 0.03 at most.  fp32: a score is the sum
+        # of 3 d_cb + 6 d_r products (three terms a query, six a RoPE product), each addition off by up to 2^-24 of a partial
+        # sum, which is about as large as the scores that count, and those are about the log-sum-exp: independent errors of
+        # 2^-24 / sqrt(3) of it in the mean, five times the root of their number (8e-5 for 192 channels and scores of 16)
+        size = max(1.0, float(np.abs(ref_lse[~empty]).max()))
+        f32_bar = 5.0 * 2.0 ** -24 / np.sqrt(3.0) * np.sqrt(3.0 * d_cb + 6.0 * d_r) * size + 1e-6
+        assert np.abs(lse[~empty] - ref_lse[~empty]).max() <= (3e-2 if dtype == "bf16" else f32_bar)
+    for s, n in enumerate(lens):
+        for j in range(q_len):
+            if n - (q_len - 1 - j) <= 0:
+                assert np.all(got[s, j] == 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [64, 16, 1, 7, 48, 256])
+def test_lengths_and_pages(dtype, page):
+    _check([0, 1, 2, 63, 64, 65, 129, 300], page=page, dtype=dtype, h=32, n_blocks=2, d_h=32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d_cb,d_r,n_blocks", [(32, 32, 1), (64, 32, 4), (96, 7, 2), (128, 64, 4), (160, 128, 1), (256, 64, 2),
+                                               (288, 33, 1), (512, 64, 1), (512, 128, 2), (128, 1, 3)])
+def test_channels(dtype, d_cb, d_r, n_blocks):
+    _check([100, 5, 333], n_blocks=n_blocks, d_cb=d_cb, d_r=d_r, h=20, d_h=48, dtype=dtype, page=32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h", [1, 3, 16, 17, 31, 33, 64, 65, 127, 128, 200])
+def test_heads(dtype, h):
+    _check([70, 200], n_blocks=2, h=h, d_h=32 if h != 128 else 128, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("groups,n_blocks,d_cb,h", [(2, 4, 128, 128), (2, 2, 256, 128), (2, 4, 64, 6), (2, 2, 128, 2)])
+def test_head_groups(dtype, groups, n_blocks, d_cb, h):
+    _check([0, 300, 64, 1], groups=groups, n_blocks=n_blocks, d_cb=d_cb, h=h, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype,h,groups,n_blocks,d_cb", [("bf16", 128, 1, 4, 128), ("f32", 128, 1, 4, 128), ("bf16", 64, 2, 2, 128),
+                                                          ("bf16", 128, 1, 1, 512), ("f32", 12, 1, 2, 64)])
+@pytest.mark.parametrize("q_len", [2, 3, 5])
+def test_query_tokens(dtype, h, groups, n_blocks, d_cb, q_len):
+    _check([0, 1, 2, 3, 4, 65, 400], q_len=q_len, h=h, groups=groups, n_blocks=n_blocks, d_cb=d_cb, dtype=dtype, gated=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_gate_scale_and_output_types(dtype, out):
+    _check([130, 64, 7], dtype=dtype, out=out, gated=True, out_scale=0.5, single=True)
+    _check([130, 64, 7], dtype=dtype, out=out, h=40, d_h=20, gated=True, out_scale=2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,n_blocks,h", [([5000], 4, 128), ([3000, 1, 0, 2900], 1, 64), ([4097, 130], 2, 16)])
+def test_long_contexts_in_chunks(dtype, lens, n_blocks, h):
+    _check(lens, n_blocks=n_blocks, h=h, dtype=dtype, page=128)
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(3)
+    _check(rng.integers(0, 200, size=70).tolist(), n_blocks=2, h=64, d_h=32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_table_much_wider_than_the_lengths(dtype):
+    _check([70, 3, 300], max_pages=5000, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_of_any_size(dtype):
+    """One token far above the others (queries a thousand times as large), and a first token far below the rest."""
+    lens, tau = [500, 65], 1.0 / np.sqrt(192)
+    hc = HostCache(lens, 2, 128, 64, dtype, 64, 8)
+    rng = np.random.default_rng(10)
+    (qa, qa64), (qr, qr64), (wv, wv64) = queries(rng, 2, 1, 2, 32, 1, 128, 64, 128, dtype)
+    big, big64 = stored(qa64 * 1024.0, dtype)
+    got = mlra.mlra_mx4_decode_attn(hc.device(), big, qr, wv, tau, out_dtype=torch.float32).double().cpu().numpy()
+    ref, _ = orc.attend(hc.rows, hc.ropes, lens, big64, qr64, wv64, tau)
+    # the weights are those of the few largest scores; a score of 10^3 is off by up to 2^-8 (2^-24) of the root sum of
+    # squares of its terms, which can move weight between tokens that are nearer to each other than that: fp32 1e-4 (a score
+    # moved by 10^3 2^-24), bf16 not compared but finite and inside the values' range
+    assert np.isfinite(got).all()
+    if dtype == "f32":
+        assert max_rel_err(got, ref) <= 1e-3
+    else:
+        assert np.abs(got).max() <= 4.0 * np.abs(ref).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nan_rows_reach_their_sequence_only(dtype):
+    lens = [100, 80]
+    hc = HostCache(lens, 2, 64, 32, dtype, 32, 9)
+    p, slot = hc.table[0, 50 // 32], 50 % 32
+    hc.scales[p, 1, slot, 0] = 255
+    rng = np.random.default_rng(11)
+    (qa, _), (qr, _), (wv, _) = queries(rng, 2, 1, 2, 16, 1, 64, 32, 32, dtype)
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, 0.1)
+    assert got[0].isnan().all() and got[1].isfinite().all()
+
+
+def test_lengths_beyond_the_capacity_count_as_the_capacity():
+    hc = HostCache([128, 64], 2, 64, 32, "f32", 64, 12)
+    hc.table[1, 1] = hc.table[0, 1]
+    rng = np.random.default_rng(13)
+    (qa, _), (qr, _), (wv, _) = queries(rng, 2, 1, 2, 16, 1, 64, 32, 32, "f32")
+    want = mlra.mlra_mx4_decode_attn(hc.device([128, 128]), qa, qr, wv, 0.1)
+    assert torch.equal(mlra.mlra_mx4_decode_attn(hc.device([129, 2 ** 31 - 1]), qa, qr, wv, 0.1), want)
+
+
+def test_unaligned_queries():
+    hc = HostCache([130, 64], 2, 64, 32, "bf16", 64, 14)
+    rng = np.random.default_rng(15)
+    (qa, _), (qr, _), (wv, _) = queries(rng, 2, 1, 2, 16, 1, 64, 32, 32, "bf16")
+    want = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, 0.1)
+
+    def shift(t):
+        flat = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
+        flat[1:] = t.flatten()
+        return flat[1:].view(t.shape)
+
+    assert torch.equal(mlra.mlra_mx4_decode_attn(hc.device(), shift(qa), shift(qr), shift(wv), 0.1), want)
