@@ -1112,8 +1112,11 @@ bool decode_mfma_supported(const DecodeArgs& a) {
 }
 
 // Blocks that serve at most 64 heads in their last 128-head group leave half of the plain form's waves
-// idle; with an even number of blocks the PAIRED form runs two blocks per workgroup instead.
-bool decode_mfma_paired(int h, int n_blocks) { return n_blocks % 2 == 0 && (h - 1) % kHeadsWG < 64; }
+// idle; with an even number of blocks in a head group the PAIRED form runs two blocks per workgroup instead (its workgroups
+// take the RoPE queries of one group).
+bool decode_mfma_paired(int h, int n_blocks, int groups) {
+  return n_blocks / groups % 2 == 0 && (h - 1) % kHeadsWG < 64;
+}
 
 // GLA-2 shape: latent heads of 256 channels (Section 2.3); 64 heads per workgroup.
 bool decode_gla_supported(const DecodeArgs& a) {
@@ -1166,7 +1169,7 @@ int launch_decode_gla(const DecodeArgs& a) {
 int launch_decode_mfma(const DecodeArgs& a) {
   static PerDeviceSetup setup;
   int setup_dev = -1;
-  const bool paired = decode_mfma_paired(a.h, a.n_blocks);
+  const bool paired = decode_mfma_paired(a.h, a.n_blocks, a.groups);
   const int lds = paired ? kStagesPaired * (2 * kLatBytes + kRopeBytes) : kStages * kStageBytes;
   if (setup.needed(&setup_dev)) {
     if (hipFuncSetAttribute((const void*)decode_mfma_kernel<kStages, 0>,

@@ -46,10 +46,11 @@ SplitPlan plan_splits(int batch, int n_blocks, int max_seq_len, int cus);
 
 // Workgroups per (sequence, chunk): the MLRA kernels run one per latent block, the MLA kernel (one
 // 512-dim latent) one per 64 heads.
-static SplitPlan plan_decode(int batch, int h, int n_blocks, int d_cb, int max_seq_len, int cus) {
-  int groups = (n_blocks == 1 && d_cb == 512) ? (h + 63) / 64 : n_blocks;
-  if (d_cb == 128 && decode_mfma_paired(h, n_blocks)) groups = n_blocks / 2;   // two blocks per workgroup
-  SplitPlan p = plan_splits(batch, groups, max_seq_len, cus);
+static SplitPlan plan_decode(int batch, int h, int groups, int n_blocks, int d_cb, int max_seq_len, int cus) {
+  int per_unit = (n_blocks == 1 && d_cb == 512) ? (h + 63) / 64 : n_blocks;
+  const bool paired = d_cb == 128 && decode_mfma_paired(h, n_blocks, groups);
+  if (paired) per_unit = n_blocks / 2;   // two blocks per workgroup
+  SplitPlan p = plan_splits(batch, per_unit, max_seq_len, cus);
   // Split mode on the MFMA MLRA shape with long chunks: twice the chunk slots, so that long sequences of
   // a ragged batch can take more chunks than short ones (the decode entry decides per call whether it
   // uses them).  The planning kernel and the round of idle slots cost 6-9 us whatever the batch looks
@@ -67,11 +68,11 @@ static SplitPlan plan_decode(int batch, int h, int n_blocks, int d_cb, int max_s
   // first; a batch of nearly equal lengths is left uncut.
   // (The MLA kernels that take planned launches, the pipelined and the four-stage one, run one workgroup per CU as well.)
   const bool mla = n_blocks == 1 && d_cb == 512;
-  const bool two_per_wg = (d_cb == 128 && decode_mfma_paired(h, n_blocks)) || d_cb == 256;
-  const long wgs = (long)batch * groups;
+  const bool two_per_wg = paired || d_cb == 256;
+  const long wgs = (long)batch * per_unit;
   if ((mla || two_per_wg) && p.n_splits == 1 && p.target_chunks == 0 && 2 * wgs > cus &&
       wgs < 2 * cus && max_seq_len >= 2048 && batch <= 512) {
-    p.target_chunks = (int)std::max<long>(batch, 2L * cus / groups);
+    p.target_chunks = (int)std::max<long>(batch, 2L * cus / per_unit);
     p.n_splits = 4;
     p.single_if_uniform = true;
   }
@@ -185,7 +186,7 @@ static int decode_common(const mlra_cache* c, int batch, int h, int groups, int 
   const int max_seq_len = c->max_pages_per_seq * c->page_size;
   DecodeArgs a;
   a.cus = device_cu_count();
-  a.plan = plan_decode(batch, h, c->n_blocks, c->d_cb, max_seq_len, a.cus);
+  a.plan = plan_decode(batch, h, groups, c->n_blocks, c->d_cb, max_seq_len, a.cus);
   const size_t need = decode_ws_bytes(batch, h, c->n_blocks, c->d_cb, a.plan);
   if (!workspace || workspace_bytes < need) return MLRA_ERR_WORKSPACE;
   if (((uintptr_t)workspace) % 256 != 0) return MLRA_ERR_WORKSPACE;
@@ -444,7 +445,7 @@ int mlra_absorb_q_folded(int32_t batch, int32_t h, int32_t d_h, int32_t n_blocks
 
 size_t mlra_decode_workspace_bytes(int32_t batch, int32_t h, int32_t n_blocks, int32_t d_cb, int32_t max_seq_len) {
   if (batch <= 0 || h <= 0 || n_blocks <= 0 || d_cb <= 0 || max_seq_len <= 0) return 0;
-  return decode_ws_bytes(batch, h, n_blocks, d_cb, plan_decode(batch, h, n_blocks, d_cb, max_seq_len, device_cu_count()));
+  return decode_ws_bytes(batch, h, n_blocks, d_cb, plan_decode(batch, h, 1, n_blocks, d_cb, max_seq_len, device_cu_count()));
 }
 
 int mlra_decode_attn(const mlra_cache* cache, int32_t batch, int32_t h, int32_t d_h, const void* q_abs,
@@ -542,7 +543,7 @@ int mlra2_absorb_q_folded(int32_t batch, int32_t h, int32_t d_h, int32_t n_block
 size_t mlra2_decode_workspace_bytes(int32_t batch, int32_t h, int32_t n_blocks, int32_t d_cb, int32_t max_seq_len) {
   if (batch <= 0 || h <= 0 || n_blocks <= 0 || d_cb <= 0 || max_seq_len <= 0) return 0;
   if (h % 2 != 0 || n_blocks % 2 != 0) return 0;
-  return decode_ws_bytes(batch, h / 2, n_blocks, d_cb, plan_decode(batch, h / 2, n_blocks, d_cb, max_seq_len, device_cu_count()));
+  return decode_ws_bytes(batch, h / 2, n_blocks, d_cb, plan_decode(batch, h / 2, 2, n_blocks, d_cb, max_seq_len, device_cu_count()));
 }
 
 int mlra2_decode_attn(const mlra_cache* cache, int32_t batch, int32_t h, int32_t d_h, const void* q_abs,
@@ -610,7 +611,7 @@ static int shape_args(DecodeArgs& a, int batch, int q_len, int h, int d_h, int g
   a.max_pages = (int)pages;
   a.dtype = dtype;
   a.cus = device_cu_count();
-  a.plan = plan_decode(a.batch, a.h, n_blocks, d_cb, a.max_pages * page_size, a.cus);
+  a.plan = plan_decode(a.batch, a.h, groups, n_blocks, d_cb, a.max_pages * page_size, a.cus);
   return MLRA_OK;
 }
 
@@ -621,7 +622,7 @@ int mlra_decode_plan_info(int32_t batch, int32_t h, int32_t d_h, int32_t groups,
   const int st = shape_args(a, batch, 1, h, d_h, groups, n_blocks, d_cb, d_r, page_size, max_seq_len, dtype);
   if (st != MLRA_OK) return st;
   const Route r = choose_route(a);
-  info[0] = r.kernel == kMlra && decode_mfma_paired(a.h, n_blocks) ? 2 : (int)r.kernel;
+  info[0] = r.kernel == kMlra && decode_mfma_paired(a.h, n_blocks, groups) ? 2 : (int)r.kernel;
   info[1] = a.plan.n_splits;
   info[2] = a.plan.chunk_tokens;
   info[3] = a.plan.target_chunks;

@@ -150,7 +150,7 @@ bool mla_mfma_fits_chunks(const DecodeArgs& a);   // for `fitted`
 int mla_mfma_stages(const DecodeArgs& a);         // which kernel: 0 the pipelined one, 2 or 4 the one with that many stages
 int launch_mla_mfma(const DecodeArgs& a);
 bool decode_mfma_supported(const DecodeArgs& a);
-bool decode_mfma_paired(int h, int n_blocks);
+bool decode_mfma_paired(int h, int n_blocks, int groups);
 bool decode_gla_supported(const DecodeArgs& a);   // 256-channel latent heads (GLA-2)
 int launch_decode_gla(const DecodeArgs& a);   // two blocks x 64 heads per workgroup instead of one x 128
 int launch_decode_mfma(const DecodeArgs& a);
