@@ -299,8 +299,7 @@ MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, in
  *   softmax_scale: tau > 0, or MLRA_SCALE_FOLDED for queries from mlra_absorb_q_folded / mlra2_absorb_q_folded
  * The arithmetic is that of a cache of type dtype that holds the same values: bf16 rounds the probabilities and the merged
  * values to bf16, fp32 rounds nothing to fewer than 24 bits.  A query without a row gives zeros and lse = -inf.  d_cb <= 512,
- * d_r <= 128; pages, lengths and page ids as for mlra_decode_attn (lengths beyond the capacity count as the capacity).
- * Deterministic. */
+ * d_r <= 128; preconditions on pages and lengths as for mlra_decode_attn.  Deterministic. */
 MLRA_API int mlra_mx4_decode_attn(const mlra_mx4_cache* cache, int32_t batch, int32_t q_len, int32_t h, int32_t d_h,
                          int32_t groups, const void* q_abs, const void* q_rope, const void* w_uv, const void* gate,
                          float softmax_scale, float out_scale, void* out, int32_t out_dtype, float* lse, void* workspace,

@@ -31,8 +31,14 @@
 // them (a + b and b + a are the same float, so both hold identical scores and take identical softmax
 // decisions), and each then accumulates Z for its own 128 channels.  Three stages of 40 KiB plus a
 // 32 KiB exchange buffer; two workgroup barriers per tile.
+//
+// MX4, for the latent cache in 4 bits (plain and PAIRED form): the stages hold the codes and scales as they lie in memory
+// (13 or 17 KiB) and a ring of three tiles holds the latent channels widened to bf16, which is exact.  Each wave widens the
+// 16 rows that it has loaded itself, tile j + 2 during the scores of step j, so that the wait for its own loads is enough;
+// the step's barrier hands the rows to the others.
 #include "chunk_fit.h"
 #include "mfma_tile.h"
+#include "mx4_tile.h"
 
 #include <type_traits>
 
@@ -238,16 +244,20 @@ __device__ __forceinline__ f32x4 acc_read4() {
 // 16-tile launch of 16 sequences of 16K tokens.
 constexpr int kFitOverhead = 10;
 
-template <int STAGES, int MODE>   // MODE 0: plain, 1: PAIRED, 2: GLA (see the head of the file)
+template <int STAGES, int MODE, bool MX4>   // MODE 0: plain, 1: PAIRED, 2: GLA (see the head of the file)
 __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool PAIRED = MODE != 0;                        // two 128-channel latent tiles per stage, 64 heads
   constexpr bool GLA = MODE == 2;                           // ... that are the halves of one 256-channel block
   constexpr int kLatRow = GLA ? 2 * kDcb * 2 : kDcb * 2;    // bytes of one cached latent row of a block
   constexpr int kBlocksWG = PAIRED ? 2 : 1;                 // latent tiles that share a stage
-  constexpr int kRopeOff = kBlocksWG * kLatBytes;           // RoPE tile behind the latent tile(s)
-  constexpr int kStageB = kRopeOff + kRopeBytes;            // 24 KiB, or 40 KiB
-  constexpr int kLoadsTile = 4 * kBlocksWG + 2;             // direct-to-LDS loads per wave and tile
+  constexpr int kRowB = MX4 ? kDcb / 2 : kLatRow;           // ... as it is cached
+  constexpr int kRawBytes = kTile * kRowB;                  // (MX4) codes of one block's tile; 1 KiB of scales behind them
+  constexpr int kRopeOff = MX4 ? kBlocksWG * kRawBytes + 1024 : kBlocksWG * kLatBytes;   // RoPE tile behind the latent tile(s)
+  constexpr int kStageB = kRopeOff + kRopeBytes;            // 24 KiB, or 40 KiB (MX4: 13 or 17)
+  constexpr int kLoadsTile = MX4 ? kBlocksWG + 3 : 4 * kBlocksWG + 2;   // direct-to-LDS loads per wave and tile
+  constexpr int kRingTile = MX4 ? kBlocksWG * kLatBytes : 0;   // (MX4) one tile of the bf16 ring, in front of the stages
+  constexpr int kRing = 3 * kRingTile;
   constexpr int kHeadsPerWG = PAIRED ? 64 : kHeadsWG;
   // Workgroup -> (sequence, chunk, block, head group).  The workgroups of one (sequence, chunk) read the
   // same RoPE rows (and, across head groups, the same latent rows).  Workgroup ids go round-robin over
@@ -319,10 +329,11 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // the 16 lanes that a 128-bit LDS read serves together then hit 16 different bank groups.
   constexpr int kQRopeRows = PAIRED ? 64 : kHeadsWG;
   constexpr int kQBytes = kHeadsWG * (kDcb * 2) + kQRopeRows * (kDr * 2);     // 48 KiB, or 40 KiB
-  constexpr int kQStages = (kQBytes + kStageB - 1) / kStageB;                 // stages the queries occupy
+  constexpr int kQStages = MX4 ? 0 : (kQBytes + kStageB - 1) / kStageB;       // stages the queries occupy (MX4: the ring)
   const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+  const unsigned stage_base = lds_base + kRing;
   const unsigned wave_u = __builtin_amdgcn_readfirstlane(wave);
-  const unsigned q_lds = lds_base + STAGES * kStageB - kQBytes;
+  const unsigned q_lds = MX4 ? lds_base : lds_base + STAGES * kStageB - kQBytes;
   const int grp_head0 = (blk0 / (p.n_blocks / p.groups)) * p.h;   // first head of this block's group in q_rope
   {
 #pragma unroll
@@ -390,11 +401,17 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   for (int q = 0; q < 2; ++q)
     rope_voff[q] = (lane >> 3) * (kDr * 2) + (((lane & 7) ^ rope_swz(8 * q + (lane >> 3))) << 4);
   // (bytes of one page: below 2^32, checked by the launcher, so page id x bytes is one 32 x 32 -> 64 bit product)
-  const unsigned lat_page_bytes = (unsigned)p.n_blocks * (unsigned)p.page_size * (unsigned)kLatRow;
+  const unsigned lat_page_bytes = (unsigned)p.n_blocks * (unsigned)p.page_size * (unsigned)kRowB;
   const unsigned rope_page_bytes = (unsigned)p.page_size * (unsigned)(kDr * 2);
-  const size_t lat_plane_bytes = (size_t)p.page_size * kLatRow;        // one block's rows inside a page
+  const size_t lat_plane_bytes = (size_t)p.page_size * kRowB;          // one block's rows inside a page
   const size_t lat_half_step = GLA ? kDcb * 2 : lat_plane_bytes;       // from the first latent tile's source to the second's
   const char* lat_blk = (const char*)p.latent + (size_t)blk0 * lat_plane_bytes;
+  // (MX4: a lane loads 16 bytes of codes, row lane / 4, and the four scales of row lane % 16, PAIRED lanes 16 .. 31 those of
+  // the second block)
+  constexpr int kScaleRow = kDcb / mx4_tile::kGroup;
+  const unsigned sc_page_bytes = (unsigned)p.n_blocks * (unsigned)p.page_size * (unsigned)kScaleRow;
+  const unsigned sc_plane = PAIRED ? ((lane >> 4) & 1) * (unsigned)p.page_size * (unsigned)kScaleRow : 0u;
+  const char* sc_blk = (const char*)p.scales + (size_t)blk0 * p.page_size * kScaleRow;
   // slot, inside its page, of this wave's first row of the next full tile to issue (they go in order)
   int issue_slot = (t0 + 16 * (int)wave_u) % p.page_size;
   int issue_stage = 0;
@@ -403,17 +420,27 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // address work), six loads, issue_end (bookkeeping, next page id).
   const char* iss_lat = nullptr;
   const char* iss_rope = nullptr;
+  const char* iss_sc = nullptr;
   unsigned iss_stage = 0;
   auto issue_begin = [&](unsigned stage_off) {   // stage_off: byte offset of the stage that receives the tile
     const unsigned page = (unsigned)issue_page;
     // start of this wave's 16 latent rows (block plane blk0) and RoPE rows of the tile inside the page
-    iss_lat = lat_blk + (unsigned long long)page * lat_page_bytes + (unsigned)issue_slot * (unsigned)kLatRow;
+    iss_lat = lat_blk + (unsigned long long)page * lat_page_bytes + (unsigned)issue_slot * (unsigned)kRowB;
+    if (MX4) iss_sc = sc_blk + (unsigned long long)page * sc_page_bytes + (unsigned)issue_slot * (unsigned)kScaleRow;
     iss_rope = (const char*)p.rope + (unsigned long long)page * rope_page_bytes + (unsigned)issue_slot * (unsigned)(kDr * 2);
-    iss_stage = lds_base + stage_off;
+    iss_stage = stage_base + stage_off;
   };
-  // parts 0..3 = latent loads (PAIRED: 4..7 = the second block's), then two RoPE loads
+  // parts 0..3 = latent loads (PAIRED: 4..7 = the second block's; MX4: codes of each block, then scales), then two RoPE loads
   auto issue_full_part = [&](int part) {
-    if (part < 4 * kBlocksWG) {
+    if (MX4 && part <= kBlocksWG) {
+      if (part < kBlocksWG) {
+        set_m0(iss_stage + part * kRawBytes + wave_u * 1024);
+        lds_dma16<0>(iss_lat + part * lat_plane_bytes, lane * 16);
+      } else {
+        set_m0(iss_stage + kBlocksWG * kRawBytes + wave_u * 256);
+        lds_dma4(iss_sc, (lane & 15) * kScaleRow + sc_plane);
+      }
+    } else if (!MX4 && part < 4 * kBlocksWG) {
       const int jb = part >> 2, q = part & 3;
       const char* src = iss_lat + jb * lat_half_step;
       if (q == 0) set_m0(iss_stage + jb * kLatBytes + wave_u * 4096);
@@ -422,7 +449,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       if (q == 2) lds_dma16<2048>(src, lat_voff[2]);
       if (q == 3) lds_dma16<3072>(src, lat_voff[3]);
     } else {
-      const int q = part - 4 * kBlocksWG;
+      const int q = part - (kLoadsTile - 2);
       if (q == 0) set_m0(iss_stage + kRopeOff + wave_u * 2048);
       if (q == 0) lds_dma16<0>(iss_rope, rope_voff[0]);
       if (q == 1) lds_dma16<1024>(iss_rope, rope_voff[1]);
@@ -456,11 +483,21 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     const int tok = t0 + (ntiles - 1) * kTile + first;
     const int idx = tok / p.page_size, slot = tok - idx * p.page_size;
     const unsigned page = (unsigned)pt_row[idx];
-    const char* src_lat = lat_blk + (unsigned long long)page * lat_page_bytes + (unsigned)slot * (unsigned)kLatRow;
+    const char* src_lat = lat_blk + (unsigned long long)page * lat_page_bytes + (unsigned)slot * (unsigned)kRowB;
     const char* src_rope = (const char*)p.rope + (unsigned long long)page * rope_page_bytes + (unsigned)slot * (unsigned)(kDr * 2);
-    const unsigned stage = lds_base + issue_stage * kStageB;
+    const unsigned stage = stage_base + issue_stage * kStageB;
+    if (MX4) {
 #pragma unroll
-    for (int jb = 0; jb < kBlocksWG; ++jb)
+      for (int jb = 0; jb < kBlocksWG; ++jb) {
+        set_m0(stage + jb * kRawBytes + wave_u * 1024);
+        lds_dma16<0>(src_lat + jb * lat_half_step, (unsigned)(min(w0 + (lane >> 2), last) - first) * kRowB + (lane & 3) * 16);
+      }
+      set_m0(stage + kBlocksWG * kRawBytes + wave_u * 256);
+      lds_dma4(sc_blk + (unsigned long long)page * sc_page_bytes + (unsigned)slot * (unsigned)kScaleRow,
+               (unsigned)(min(w0 + (lane & 15), last) - first) * kScaleRow + sc_plane);
+    }
+#pragma unroll
+    for (int jb = 0; jb < (MX4 ? 0 : kBlocksWG); ++jb)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int t = (wave * 4 + q) * 4 + (lane >> 4);          // 0..63
@@ -519,13 +556,14 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_ptr;
   typedef const __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
   // K operand ks (this wave's 32 token rows x 16 channels) of the tile in the stage at byte offset st_off
-  auto load_k_part = [&](unsigned st_off, int ks, bf16x8 (&ka)[12]) {
-    const unsigned base = lds_base + st_off + (ks < 8 ? k_lat_off : k_rope_off);
+  // (lat_off: where its latent channels are, the stage itself or the ring's tile)
+  auto load_k_part = [&](unsigned st_off, unsigned lat_off, int ks, bf16x8 (&ka)[12]) {
+    const unsigned base = ks < 8 ? lds_base + lat_off + k_lat_off : stage_base + st_off + k_rope_off;
     ka[ks] = *(lds_bf16x8_ptr)(size_t)(base ^ ((ks & 7) << 5));
   };
-  auto load_k = [&](unsigned st_off, bf16x8 (&ka)[12]) {
+  auto load_k = [&](unsigned st_off, unsigned lat_off, bf16x8 (&ka)[12]) {
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks) load_k_part(st_off, ks, ka);
+    for (int ks = 0; ks < 12; ++ks) load_k_part(st_off, lat_off, ks, ka);
   };
   // transposed V operand (32 channels of tile mt x 16 of this wave's token rows) of the tile in that stage
   auto load_v_part = [&](unsigned st_off, int ss, int mt, bf16x8 (&va)[2][4]) {
@@ -536,6 +574,46 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     const short4v lo = lds_tr16(lo_p + ss * 16 * (kDcb * 2));
     const short4v hi = lds_tr16(hi_p + ss * 16 * (kDcb * 2));
     va[ss][mt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // (MX4) Widening of the wave's own 16 rows of a tile: unit u = 4 jb + i is the rows 4 i .. 4 i + 3 of block jb, a lane has
+  // eight channels (row lane / 16, 16-byte chunk lane % 16 of the bf16 row).  Reads are linear; the chunks of a row that
+  // sixteen lanes write lie in sixteen different bank groups.
+  constexpr int kUnits = MX4 ? 4 * kBlocksWG : 0;
+  const unsigned cv_codes = wave * 1024 + lane * 4;
+  const unsigned cv_scale = kBlocksWG * kRawBytes + wave * 256 + (lane >> 4) * kScaleRow + ((lane >> 2) & 3);
+  const unsigned cv_out = (16 * wave + (lane >> 4)) * (kDcb * 2) + (((lane & 15) ^ ((lane >> 4) << 2)) << 4);
+  unsigned cv_raw[8], cv_byte[8];
+  mx4_tile::u32x4 cv_val;
+  auto widen_read = [&](unsigned st_off, int u) {
+    typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
+    const int jb = u >> 2, i = u & 3;
+    cv_raw[u] = *(u32_ptr)(size_t)(stage_base + st_off + cv_codes + jb * kRawBytes + i * 256);
+    cv_byte[u] = *(lds_byte_ptr)(size_t)(stage_base + st_off + cv_scale + jb * 64 + i * 16);
+  };
+  auto widen_half = [&](int u, int half) {       // four of the eight channels
+    const float scale = mx4_tile::scale_of(cv_byte[u]);
+    if (half == 0) {
+      cv_val[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 0));
+      cv_val[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 1));
+    } else {
+      cv_val[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 2));
+      cv_val[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 3));
+    }
+  };
+  auto widen_write = [&](unsigned lat_off, int u) {
+    typedef __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
+    const int jb = u >> 2, i = u & 3;
+    *(u32x4_ptr)(size_t)(((lds_base + lat_off + cv_out) ^ (i << 4)) + jb * kLatBytes + i * 1024) = cv_val;
+  };
+  auto widen_tile = [&](unsigned st_off, unsigned lat_off) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) widen_read(st_off, u);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      widen_half(u, 0);
+      widen_half(u, 1);
+      widen_write(lat_off, u);
+    }
   };
   // Column maxima.  In the accumulator layout a lane holds 16 of the 32 token rows of its head column
   // and the lane 32 away holds the other 16.  max8 folds eight more rows into a running maximum;
@@ -708,11 +786,18 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   __builtin_amdgcn_s_barrier();
   for (int jj = STAGES - kQStages; jj < STAGES && jj < ntiles; ++jj) issue_tile();
   if (ntiles >= STAGES) wait_vmcnt<kLoadsTile * (STAGES - 2)>(); else wait_vmcnt<0>();
+  if (MX4) {
+    asm volatile("" ::: "memory");
+    widen_tile(0, 0);
+    widen_tile((1 % STAGES) * kStageB, kRingTile);   // (whatever the stage holds if the chunk has a single tile)
+    wait_vm_lgkm<63>();
+    asm volatile("" ::: "memory");
+  }
   __builtin_amdgcn_s_barrier();   // tiles 0 and 1 landed for every wave
   f32x16 sa0, sa1, sb0, sb1;
   bf16x8 ka[12];
   {
-    load_k(0, ka);
+    load_k(0, 0, ka);
 #pragma unroll
     for (int i = 0; i < 16; ++i) { sa0[i] = 0.f; sa1[i] = 0.f; }
 #pragma unroll
@@ -757,7 +842,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     // exists); their probabilities are what has to vanish.
     if (nvalid_last < kTile) { mask_tail(sa0); mask_tail(sa1); }
     __builtin_amdgcn_sched_barrier(0);
-    load_k((1 % STAGES) * kStageB, ka);   // (a stale stage if the chunk has a single tile: those scores are never used)
+    load_k((1 % STAGES) * kStageB, MX4 ? kRingTile : (1 % STAGES) * kStageB, ka);   // (a stale stage if the chunk has a single tile: those scores are never used)
   }
 
   // ---- main loop, software-pipelined over tiles; every MFMA is followed by about six issue slots of
@@ -774,15 +859,29 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // straight-line code; the last STAGES steps of a chunk issue nothing.  sched_barrier(0) pins the
   // interleaving. ----
   // (the ring position is kept as a byte offset: no multiplication per step.  A step's loads go into the
-  // stage of the tile it consumes, tile j + STAGES into the stage of tile j.)
-  unsigned st_cur = 0;
+  // stage of the tile it consumes, tile j + STAGES into the stage of tile j.  MX4: the stage of tile j + 1 is free as well, its
+  // codes are widened and its RoPE rows were read in the previous step, and takes tile j + 1 + STAGES; tile STAGES goes out
+  // here.)
+  unsigned st_cur = 0, ring_cur = 0;
+  if (MX4) {
+    wait_vm_lgkm<63>();
+    __builtin_amdgcn_s_barrier();
+    if (ntiles > STAGES) issue_tile();
+  }
   auto step = [&](auto issue_tag, int j, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
     constexpr bool ISSUE = decltype(issue_tag)::value;   // tile j + STAGES exists (and is a full one)
     const bool has_next = j + 1 < ntiles;
     const unsigned st_k2 = (st_cur + 2 * kStageB >= STAGES * kStageB) ? st_cur + 2 * kStageB - STAGES * kStageB
                                                                        : st_cur + 2 * kStageB;   // stage of tile j+2
+    const unsigned st_next = st_cur + kStageB == STAGES * kStageB ? 0 : st_cur + kStageB;
+    const unsigned ring_k2 = ring_cur + 2 * kRingTile >= kRing ? ring_cur + 2 * kRingTile - kRing : ring_cur + 2 * kRingTile;
+    const unsigned lat_cur = MX4 ? ring_cur : st_cur, lat_k2 = MX4 ? ring_k2 : st_k2;
 
     __builtin_amdgcn_sched_barrier(0);
+    if (MX4) {   // this wave's loads of tile j+2 have landed (tiles j+3 .. j+STAGES may be in flight)
+      if (ISSUE) wait_vmcnt<kLoadsTile * (STAGES - 2)>(); else wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+    }
     // ---- block A: 24 score MFMAs; the first of each head tile starts from minus the reference maximum.
     // MFMA i < 16 carries the exponentials of probability pair i (pairs 0..7: head tile 0, 8..15: head
     // tile 1) and the bf16 rounding of pair i-1; MFMA 16+q carries the LDS transpose reads of V operand q.
@@ -810,7 +909,16 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       }
       if (i >= 16) {
         const int q = i - 16;
-        load_v_part(st_cur, q >> 2, q & 3, va);
+        load_v_part(lat_cur, q >> 2, q & 3, va);
+      }
+      if (MX4) {
+        // units of tile j+2: read one MFMA after another, widened and written two MFMAs each once they have arrived
+        if (i < kUnits) widen_read(st_k2, i);
+        const int u = (i - 7) >> 1;
+        if (i >= 7 && u < kUnits) {
+          widen_half(u, (i - 7) & 1);
+          if ((i - 7) & 1) widen_write(lat_k2, u);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -843,14 +951,14 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       // a scalar load of the next page id; while that is in flight every wait for an LDS read has to be a wait
       // for everything, so it goes at the end of the step, where the next wait is one for everything anyway:
       // measured 1745 cycles per tile there against 1785 behind the barrier and 1800 in front of it.)
-      if (m == 0 && ISSUE) issue_begin(st_cur);
+      if (m == 0 && ISSUE) issue_begin(MX4 ? st_next : st_cur);
       if (m == 14 && ISSUE && kLoadsTile <= 6) issue_end();
       if (m == 1) {
         // this wave's LDS reads of V(j) have returned (so has everything older) before it tells the
         // others that the stage may be overwritten
         // (while tiles are still being issued, STAGES - 3 of them may stay in flight behind tile j+2; the
         // last steps of a chunk simply wait for everything that is left)
-        if (ISSUE) wait_vm_lgkm<kLoadsTile * (STAGES - 3)>(); else wait_vm_lgkm<0>();
+        if (MX4) wait_vm_lgkm<63>(); else if (ISSUE) wait_vm_lgkm<kLoadsTile * (STAGES - 3)>(); else wait_vm_lgkm<0>();
         __builtin_amdgcn_s_barrier();
       }
       // (a compute unit takes about 64 bytes of vector-memory requests per cycle, and its four waves issue
@@ -885,7 +993,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       if (m == 15) hold(va[1][1]);
       if (m == 10) hold(pb0[0]);
       if (m == 11) hold(pb1[0]);
-      if (m >= 2 && m <= 13) load_k_part(st_k2, m - 2, ka);
+      if (m >= 2 && m <= 13) load_k_part(st_k2, lat_k2, m - 2, ka);
       // (the score chains ended four MFMAs and a barrier before MFMA 2; in the GLA form the partner's partial
       // scores are added behind MFMAs 2..5 first)
       constexpr int kMaxAt = GLA ? 6 : 2;
@@ -911,13 +1019,15 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       rescale(std::integral_constant<int, 0>{}, need0 ? mx0 : 0.f, n0);
       rescale(std::integral_constant<int, 1>{}, need1 ? mx1 : 0.f, n1);
     }
-    st_cur = (st_cur + kStageB == STAGES * kStageB) ? 0 : st_cur + kStageB;
+    st_cur = st_next;
+    if (MX4) ring_cur = ring_cur + kRingTile == kRing ? 0 : ring_cur + kRingTile;
   };
   {
     const std::integral_constant<bool, true> issuing;
     const std::integral_constant<bool, false> draining;
     // steps 0 .. ntiles - STAGES - 1 issue a tile each, the last STAGES steps only drain the pipeline
-    const int n_issue = ntiles > STAGES ? ntiles - STAGES : 0;
+    constexpr int kAhead = MX4 ? STAGES + 1 : STAGES;
+    const int n_issue = ntiles > kAhead ? ntiles - kAhead : 0;
     int j = 0;
     for (; j + 4 <= n_issue; j += 4) {   // (four steps per trip: the taken branch at the end costs a refetch)
       step(issuing, j, sa0, sa1, sb0, sb1);
@@ -1068,6 +1178,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 
 constexpr int kStages = 6;         // plain form: 6 x 24 KiB
 constexpr int kStagesPaired = 4;   // PAIRED form: 4 x 40 KiB = all 160 KiB of LDS
+constexpr int kStagesMx4 = 8;         // MX4, plain: 8 x 13 KiB behind a ring of 48 KiB
+constexpr int kStagesPairedMx4 = 3;   // MX4, PAIRED: 3 x 17 KiB behind a ring of 96 KiB
 
 }  // namespace
 
@@ -1132,7 +1244,7 @@ int launch_decode_gla(const DecodeArgs& a) {
   constexpr int kStagesGla = 3;
   const int lds = kStagesGla * (2 * kLatBytes + kRopeBytes) + 4 * 8 * 64 * 16;   // stages + score exchange
   if (setup.needed(&setup_dev)) {
-    if (hipFuncSetAttribute((const void*)decode_mfma_kernel<kStagesGla, 2>,
+    if (hipFuncSetAttribute((const void*)decode_mfma_kernel<kStagesGla, 2, false>,
                             hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
       return MLRA_ERR_LAUNCH;
     setup.done(setup_dev);
@@ -1162,26 +1274,33 @@ int launch_decode_gla(const DecodeArgs& a) {
   const long long n_wg = (long long)a.plan.n_splits * a.n_blocks * ((a.h + 63) / 64) * a.batch;
   if (n_wg <= 0 || n_wg > 0x7fffffffLL) return MLRA_ERR_SHAPE;
   if (want_seq_order(a, n_wg) && launch_seq_order(a) == MLRA_OK) p.seq_order = a.seq_order;
-  MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<kStagesGla, 2>), dim3((unsigned)n_wg), dim3(256), lds, a.stream, p);
+  MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<kStagesGla, 2, false>), dim3((unsigned)n_wg), dim3(256), lds, a.stream, p);
+  return check_launch();
+}
+
+template <int STAGES, int MODE, bool MX4>
+static int launch_form(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) {
+  constexpr int blocks = MODE == 1 ? 2 : 1;
+  constexpr int lds = MX4 ? 3 * blocks * kLatBytes + STAGES * (blocks * kTile * kDcb / 2 + 1024 + kRopeBytes)
+                          : STAGES * (blocks * kLatBytes + kRopeBytes);
+  static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+  static PerDeviceSetup setup;
+  int dev = -1;
+  if (setup.needed(&dev)) {
+    if (hipFuncSetAttribute((const void*)decode_mfma_kernel<STAGES, MODE, MX4>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                            lds) != hipSuccess)
+      return MLRA_ERR_LAUNCH;
+    setup.done(dev);
+  }
+  MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<STAGES, MODE, MX4>), dim3(n_wg), dim3(256), lds, a.stream, p);
   return check_launch();
 }
 
 int launch_decode_mfma(const DecodeArgs& a) {
-  static PerDeviceSetup setup;
-  int setup_dev = -1;
   const bool paired = decode_mfma_paired(a.h, a.n_blocks, a.groups);
-  const int lds = paired ? kStagesPaired * (2 * kLatBytes + kRopeBytes) : kStages * kStageBytes;
-  if (setup.needed(&setup_dev)) {
-    if (hipFuncSetAttribute((const void*)decode_mfma_kernel<kStages, 0>,
-                            hipFuncAttributeMaxDynamicSharedMemorySize, kStages * kStageBytes) != hipSuccess ||
-        hipFuncSetAttribute((const void*)decode_mfma_kernel<kStagesPaired, 1>,
-                            hipFuncAttributeMaxDynamicSharedMemorySize,
-                            kStagesPaired * (2 * kLatBytes + kRopeBytes)) != hipSuccess)
-      return MLRA_ERR_LAUNCH;
-    setup.done(setup_dev);
-  }
   MfmaParams p;
   p.latent = (const bf16_t*)a.latent;
+  p.scales = (const uint8_t*)a.scales;
   p.rope = (const bf16_t*)a.rope;
   p.page_table = a.page_table;
   p.seq_lens = a.seq_lens;
@@ -1215,11 +1334,9 @@ int launch_decode_mfma(const DecodeArgs& a) {
     p.chunk_out = a.chunk_tab;
   }
   if (want_seq_order(a, n_wg) && launch_seq_order(a) == MLRA_OK) p.seq_order = a.seq_order;
-  if (paired)
-    MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<kStagesPaired, 1>), dim3((unsigned)n_wg), dim3(256), lds, a.stream, p);
-  else
-    MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<kStages, 0>), dim3((unsigned)n_wg), dim3(256), lds, a.stream, p);
-  return check_launch();
+  if (a.scales)
+    return paired ? launch_form<kStagesPairedMx4, 1, true>(a, p, (unsigned)n_wg) : launch_form<kStagesMx4, 0, true>(a, p, (unsigned)n_wg);
+  return paired ? launch_form<kStagesPaired, 1, false>(a, p, (unsigned)n_wg) : launch_form<kStages, 0, false>(a, p, (unsigned)n_wg);
 }
 
 }  // namespace mlra

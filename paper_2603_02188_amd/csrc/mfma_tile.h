@@ -47,6 +47,7 @@ struct MfmaParams {
                               // tokens less
   int cus = 0;
   int split_major = 0;        // (MLA) dispatch order: all sequences' first chunks, then all second ones, ...
+  const uint8_t* scales = nullptr;   // (latent in 4 bits) [num_pages][n_blocks][page_size][d_cb / 32]
   int rows_bf16;              // 1: part_z receives each chunk's partial as z / l rounded to bf16, [..][chunk][head][channels]
                               // (what the MFMA epilogue merges); 0: fp32 partials, not normalised (fp32 merge, MLA)
 };
@@ -83,6 +84,11 @@ __device__ __forceinline__ void set_m0(unsigned v) { asm volatile("s_mov_b32 m0,
 template <int OFF>
 __device__ __forceinline__ void lds_dma16(const void* sbase, unsigned voff) {
   asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" : : "v"(voff), "s"(sbase), "n"(OFF) : "memory");
+}
+
+// four bytes a lane, to m0 + 4 i
+__device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff) {
+  asm volatile("global_load_lds_dword %0, %1" : : "v"(voff), "s"(sbase) : "memory");
 }
 
 __device__ __forceinline__ short4v lds_tr16(const __attribute__((address_space(3))) unsigned char* p) {

@@ -133,7 +133,18 @@ static size_t decode_ws_bytes(int batch, int h, int n_blocks, int d_cb, const Sp
          align_up((size_t)batch * p.n_splits * sizeof(int32_t), 256);
 }
 
-enum DecodeKernel { kPlain = 0, kMlra = 1, kGla = 3, kMla = 4, kF32 = 5 };   // (mlra_decode_plan_info [0]; 2: kMlra, paired)
+// Where the parts of a workspace of decode_ws_bytes lie (a.batch, a.h, a.n_blocks, a.d_cb and a.plan are set).
+static void carve_workspace(DecodeArgs& a, void* workspace) {
+  const size_t units = (size_t)a.batch * a.n_blocks * a.plan.n_splits;
+  a.part_z = (float*)workspace;
+  a.part_ml = (float*)((char*)workspace + align_up(units * a.h * a.d_cb * sizeof(float), 256));
+  a.seq_order = (int32_t*)((char*)a.part_ml + align_up(units * a.h * 2 * sizeof(float), 256));
+  a.chunk_tab = (int32_t*)((char*)a.seq_order + align_up((size_t)a.batch * sizeof(int32_t), 256));
+  a.unit_tab = (int32_t*)((char*)a.chunk_tab + align_up((size_t)a.batch * sizeof(int32_t), 256));
+}
+
+// (mlra_decode_plan_info [0]; 2: kMlra, paired.  kMx4: the kernel for every shape of a cache in 4 bits)
+enum DecodeKernel { kPlain = 0, kMlra = 1, kGla = 3, kMla = 4, kF32 = 5, kMx4 = 6 };
 struct Route {
   DecodeKernel kernel;
   bool merge_mfma;   // the bf16 epilogue
@@ -149,6 +160,7 @@ struct Route {
 static Route choose_route(DecodeArgs& a) {
   Route r;
   r.kernel = decode_mfma_supported(a) ? kMlra
+             : a.scales               ? kMx4
              : decode_gla_supported(a) ? kGla
              : mla_mfma_supported(a)  ? kMla
              : decode_f32_supported(a) ? kF32
@@ -164,6 +176,37 @@ static Route choose_route(DecodeArgs& a) {
   r.planned = !a.fitted && a.plan.target_chunks > 0 && r.merge_mfma &&
               (r.kernel == kMlra || r.kernel == kGla || r.kernel == kMla);
   return r;
+}
+
+// The launches of a decode call.  Rooms: q_group > 1 query tokens per sequence take a row of the lengths and of the page table
+// each where the kernels want them.
+static int run_decode(DecodeArgs& a, const Route& r, int32_t* lens_room, int32_t* table_room) {
+  if (a.q_group > 1 && !a.fitted) {
+    const int st = launch_expand_queries(a.seq_lens, a.page_table, a.batch / a.q_group, a.q_group, a.max_pages, lens_room,
+                                         table_room, a.stream);
+    if (st != MLRA_OK) return st;
+    a.seq_lens = lens_room;
+    a.page_table = table_room;
+  }
+  if (r.planned) a.balanced = launch_plan_chunks(a) == MLRA_OK;
+  // the MLRA MFMA kernels hand the epilogue normalised bf16 rows (one per chunk) instead of fp32 partials
+  a.rows_bf16 = r.merge_mfma && (r.kernel == kMlra || r.kernel == kGla);
+  // the MFMA launchers record their kernel's own start and end; the others are bracketed by stream markers
+  const bool main_fast = r.kernel == kMlra || r.kernel == kGla || r.kernel == kMla, epi_fast = r.merge_mfma;
+  if (a.t_main.on() && !main_fast) (void)hipEventRecord(a.t_main.start, a.stream);
+  int st = r.kernel == kMlra ? launch_decode_mfma(a)
+           : r.kernel == kGla ? launch_decode_gla(a)
+           : r.kernel == kMla ? launch_mla_mfma(a)
+           : r.kernel == kF32 ? launch_decode_f32(a)
+           : r.kernel == kMx4 ? launch_mx4_decode(a)
+                              : launch_decode_generic(a);
+  if (st != MLRA_OK) return st;
+  if (a.t_main.on() && !main_fast) (void)hipEventRecord(a.t_main.stop, a.stream);
+  if (a.t_epi.on() && !epi_fast) (void)hipEventRecord(a.t_epi.start, a.stream);
+  st = epi_fast ? launch_merge_upproj_mfma(a) : launch_merge_upproj_f32(a);
+  if (a.t_epi.on() && !epi_fast) (void)hipEventRecord(a.t_epi.stop, a.stream);
+  if (st == MLRA_OK && timing_on()) ++g_timing_calls;
+  return st;
 }
 
 // h: heads served by one block (all heads when groups == 1, the heads of one group otherwise)
@@ -190,12 +233,6 @@ static int decode_common(const mlra_cache* c, int batch, int h, int groups, int 
   const size_t need = decode_ws_bytes(batch, h, c->n_blocks, c->d_cb, a.plan);
   if (!workspace || workspace_bytes < need) return MLRA_ERR_WORKSPACE;
   if (((uintptr_t)workspace) % 256 != 0) return MLRA_ERR_WORKSPACE;
-  const size_t units = (size_t)batch * c->n_blocks * a.plan.n_splits;
-  a.part_z = (float*)workspace;
-  a.part_ml = (float*)((char*)workspace + align_up(units * h * c->d_cb * sizeof(float), 256));
-  a.seq_order = (int32_t*)((char*)a.part_ml + align_up(units * h * 2 * sizeof(float), 256));
-  a.chunk_tab = (int32_t*)((char*)a.seq_order + align_up((size_t)batch * sizeof(int32_t), 256));
-  a.unit_tab = (int32_t*)((char*)a.chunk_tab + align_up((size_t)batch * sizeof(int32_t), 256));
   a.balanced = false;
   a.fitted = false;
   a.rows_bf16 = false;
@@ -226,32 +263,8 @@ static int decode_common(const mlra_cache* c, int batch, int h, int groups, int 
   a.stream = (hipStream_t)stream;
   a.t_main = timing_pair(0);
   a.t_epi = timing_pair(1);
-  const Route r = choose_route(a);
-  if (q_group > 1 && !a.fitted) {
-    const int st = launch_expand_queries(c->seq_lens, c->page_table, batch / q_group, q_group, c->max_pages_per_seq, lens_room,
-                                         table_room, a.stream);
-    if (st != MLRA_OK) return st;
-    a.seq_lens = lens_room;
-    a.page_table = table_room;
-  }
-  if (r.planned) a.balanced = launch_plan_chunks(a) == MLRA_OK;
-  // the MLRA MFMA kernels hand the epilogue normalised bf16 rows (one per chunk) instead of fp32 partials
-  a.rows_bf16 = r.merge_mfma && (r.kernel == kMlra || r.kernel == kGla);
-  // the MFMA launchers record their kernel's own start and end; the others are bracketed by stream markers
-  const bool main_fast = r.kernel == kMlra || r.kernel == kGla || r.kernel == kMla, epi_fast = r.merge_mfma;
-  if (a.t_main.on() && !main_fast) (void)hipEventRecord(a.t_main.start, a.stream);
-  int st = r.kernel == kMlra ? launch_decode_mfma(a)
-           : r.kernel == kGla ? launch_decode_gla(a)
-           : r.kernel == kMla ? launch_mla_mfma(a)
-           : r.kernel == kF32 ? launch_decode_f32(a)
-                              : launch_decode_generic(a);
-  if (st != MLRA_OK) return st;
-  if (a.t_main.on() && !main_fast) (void)hipEventRecord(a.t_main.stop, a.stream);
-  if (a.t_epi.on() && !epi_fast) (void)hipEventRecord(a.t_epi.start, a.stream);
-  st = epi_fast ? launch_merge_upproj_mfma(a) : launch_merge_upproj_f32(a);
-  if (a.t_epi.on() && !epi_fast) (void)hipEventRecord(a.t_epi.stop, a.stream);
-  if (st == MLRA_OK && timing_on()) ++g_timing_calls;
-  return st;
+  carve_workspace(a, workspace);
+  return run_decode(a, choose_route(a), lens_room, table_room);
 }
 
 // ---- latent cache in 4 bits ---------------------------------------------------------------------------------------
@@ -274,8 +287,8 @@ static int mx4_rows_common(const mlra_mx4_cache* c, int batch, int n_rows, const
   return check_mx4_cache(c, batch);
 }
 
-// Two rounds of the decode kernel's workgroups run at a time on a compute unit.
-static SplitPlan plan_mx4(int units, int h, int n_blocks, int d_cb, int max_seq_len, int cus) {
+// The kernel for every shape runs two workgroups at a time on a compute unit, one per 64 heads at most.
+static SplitPlan plan_mx4(int units, int h, int n_blocks, int max_seq_len, int cus) {
   return plan_splits(units, n_blocks * ((h + 63) / 64), max_seq_len, 2 * cus);
 }
 
@@ -315,10 +328,11 @@ int mlra_mx4_read_kv(const mlra_mx4_cache* c, int32_t batch, int32_t n_rows, con
 size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, int32_t groups, int32_t n_blocks,
                                        int32_t d_cb, int32_t page_size, int32_t max_pages_per_seq) {
   if (!mx4_shape_ok(batch, q_len, h, groups, n_blocks, d_cb, page_size, max_pages_per_seq)) return 0;
-  const int units = batch * q_len, hb = h / groups;
+  const int units = batch * q_len, hb = h / groups, len = max_pages_per_seq * page_size, cus = device_cu_count();
+  // (whichever kernel runs: that depends on the types and on d_r as well)
   return mx4_table_bytes(units, q_len, max_pages_per_seq) +
-         decode_ws_bytes(units, hb, n_blocks, d_cb,
-                         plan_mx4(units, hb, n_blocks, d_cb, max_pages_per_seq * page_size, device_cu_count()));
+         std::max(decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4(units, hb, n_blocks, len, cus)),
+                  decode_ws_bytes(units, hb, n_blocks, d_cb, plan_decode(units, hb, groups, n_blocks, d_cb, len, cus)));
 }
 
 int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, int32_t h, int32_t d_h, int32_t groups,
@@ -339,7 +353,7 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 256 != 0) return MLRA_ERR_WORKSPACE;
   DecodeArgs a = {};
   a.cus = device_cu_count();
-  a.plan = plan_mx4(units, hb, c->n_blocks, c->d_cb, max_seq_len, a.cus);
+  a.plan = plan_decode(units, hb, groups, c->n_blocks, c->d_cb, max_seq_len, a.cus);
   a.latent = c->latent;
   a.scales = c->scales;
   a.rope = c->rope;
@@ -366,22 +380,13 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   a.q_group = q_len;
   a.dtype = c->dtype;
   a.stream = (hipStream_t)stream;
-  char* ws = (char*)workspace;
-  if (q_len > 1) {
-    int32_t* const lens = (int32_t*)ws;
-    int32_t* const table = (int32_t*)(ws + align_up((size_t)units * sizeof(int32_t), 256));
-    const int st = launch_expand_queries(c->seq_lens, c->page_table, batch, q_len, c->max_pages_per_seq, lens, table, a.stream);
-    if (st != MLRA_OK) return st;
-    a.seq_lens = lens;
-    a.page_table = table;
-    ws += mx4_table_bytes(units, q_len, c->max_pages_per_seq);
-  }
-  const size_t parts = (size_t)units * c->n_blocks * a.plan.n_splits * hb;
-  a.part_z = (float*)ws;
-  a.part_ml = (float*)(ws + align_up(parts * c->d_cb * sizeof(float), 256));
-  const int st = launch_mx4_decode(a);
-  if (st != MLRA_OK) return st;
-  return merge_upproj_mfma_supported(a) ? launch_merge_upproj_mfma(a) : launch_merge_upproj_f32(a);
+  a.t_main = timing_pair(0);
+  a.t_epi = timing_pair(1);
+  if (!decode_mfma_supported(a)) a.plan = plan_mx4(units, hb, c->n_blocks, max_seq_len, a.cus);
+  int32_t* const lens = (int32_t*)workspace;
+  int32_t* const table = (int32_t*)((char*)workspace + align_up((size_t)units * sizeof(int32_t), 256));
+  carve_workspace(a, (char*)workspace + mx4_table_bytes(units, q_len, c->max_pages_per_seq));
+  return run_decode(a, choose_route(a), lens, table);
 }
 
 const char* mlra_strerror(int status) {

@@ -107,7 +107,7 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
     hg = wg % p.n_hg;
   }
   const int b = u % p.n_blocks, s = u / p.n_blocks % p.batch, split_id = u / p.n_blocks / p.batch;
-  const int n = min(p.seq_lens[s], p.max_pages * p.page_size), t0 = split_id * p.chunk;
+  const int n = p.seq_lens[s], t0 = split_id * p.chunk;
   if (n <= 0 || (unsigned)t0 >= (unsigned)n) return;         // (slots beyond the capacity)
   const int t1 = t0 + min(n - t0, p.chunk), ntiles = (t1 - t0 + kTile - 1) / kTile;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
