@@ -29,6 +29,7 @@
 // d_cb = 512.
 #include "chunk_fit.h"
 #include "mfma_tile.h"
+#include "mx4_tile.h"
 
 #include <type_traits>
 
@@ -426,8 +427,21 @@ constexpr int kPStages = 4;
 constexpr int kPPOff = kPStages * kMStage, kPAOff = kPPOff + 2 * kMPBytes, kPXOff = kPAOff + 2 * kMHeads * 4,
               kPFOff = kPXOff + 2 * 4 * 32 * 4, kPLds = kPFOff + 2 * 4 * 4;
 static_assert(kPLds <= 160 * 1024, "one workgroup per CU");
+// Latent cache in 4 bits: the stages hold codes, scales (1 KiB) and RoPE rows as they lie in memory, 13 KiB; behind what is
+// above, a ring of three tiles holds the latent channels widened to bf16.  A wave widens the eight rows that it loaded
+// itself, tile j + 2 during the scores of step j; the barrier behind them hands the rows to the others.
+constexpr int kXRow = kMDc / 2, kXScaleRow = kMDc / mx4_tile::kGroup, kXScales = kMTok * kXRow, kXRope = kXScales + 1024,
+              kXStage = kXRope + kMRopeBytes, kXLoads = 4;
+constexpr int kXRing = kPStages * kXStage, kXShift = kXRing + 3 * kMLatBytes - kPPOff;   // (the tables move up by kXShift)
+constexpr int kXLds = kPLds + kXShift;
+static_assert(kXLds <= 160 * 1024, "one workgroup per CU");
 
+template <bool MX4>
 __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
+  constexpr int kStageB = MX4 ? kXStage : kMStage, kRopeOff = MX4 ? kXRope : kMLatBytes;
+  constexpr int kPP = kPPOff + (MX4 ? kXShift : 0), kPA = kPAOff + (MX4 ? kXShift : 0), kPX = kPXOff + (MX4 ? kXShift : 0),
+                kPF = kPFOff + (MX4 ? kXShift : 0);
+  constexpr int kLoads = MX4 ? kXLoads : kMLoads;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   int hgrp, seq, split, chunk_len;
   if (!mla_unit<true>(p, hgrp, seq, split, chunk_len)) return;
@@ -451,7 +465,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   // 0..7) and RoPE rows 8 w .. + 7 (part 8).  Tiles are issued in order, in parts that sit behind different MFMAs; the id of
   // the page after the current one is always loaded already (pages hold whole tiles).
   const const_i32_ptr pt_row = (const_i32_ptr)(p.page_table + (size_t)seq * p.max_pages);
-  const size_t lat_page_bytes = (size_t)p.page_size * (kMDc * 2);
+  const size_t lat_page_bytes = (size_t)p.page_size * (MX4 ? kXRow : kMDc * 2);
   const size_t rope_page_bytes = (size_t)p.page_size * (kDr * 2);
   int iss_tok = t0, iss_page_at = t0 / p.page_size, iss_slot = t0 % p.page_size;
   unsigned iss_page = (unsigned)pt_row[iss_page_at];
@@ -459,15 +473,38 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   unsigned lat_voff[8], rope_voff;
 #pragma unroll
   for (int i = 0; i < 8; ++i) lat_voff[i] = ((lane * 16) ^ (unsigned)(lat_swz(8 * wave + i) << 4)) + (i & 4) * 1024;
+  // (4 bits: a load moves four rows of codes, the third the scales of the wave's rows, sixteen bytes each, twice)
+  const size_t sc_page_bytes = (size_t)p.page_size * kXScaleRow;
+  const char* iss_sc = nullptr;
   rope_voff = (8 * wave + (lane >> 3)) * (kDr * 2) + (((lane * 16) & 0x70) ^ (rope_swz(8 * wave + (lane >> 3)) << 4));
   const char* iss_lat = nullptr;
   const char* iss_rope = nullptr;
   unsigned iss_dst = lds_base;
   auto issue_begin = [&]() {
-    iss_lat = (const char*)p.latent + iss_page * lat_page_bytes + (size_t)(iss_slot + 8 * wave_u) * (kMDc * 2);   // (pages of 4 GiB)
+    if (MX4) {
+      iss_lat = (const char*)p.latent + iss_page * lat_page_bytes + (size_t)iss_slot * kXRow;
+      iss_sc = (const char*)p.scales + iss_page * sc_page_bytes + (size_t)iss_slot * kXScaleRow;
+    } else {
+      iss_lat = (const char*)p.latent + iss_page * lat_page_bytes + (size_t)(iss_slot + 8 * wave_u) * (kMDc * 2);   // (pages of 4 GiB)
+    }
     iss_rope = (const char*)p.rope + iss_page * rope_page_bytes + (size_t)iss_slot * (kDr * 2);
   };
+  // part i of a tile in 4 bits, whose rows behind `last` are copies of that one
+  auto issue_part_mx4 = [&](int i, int last) {
+    if (i < 2) {
+      set_m0(iss_dst + wave_u * (8 * kXRow) + i * 1024);
+      lds_dma16<0>(iss_lat, min(8 * wave + 4 * i + (lane >> 4), last) * kXRow + (lane & 15) * 16);
+    } else if (i == 2) {
+      set_m0(iss_dst + kXScales + wave_u * 256);
+      lds_dma4(iss_sc, min(8 * wave + ((lane >> 2) & 7), last) * kXScaleRow + (lane & 3) * 4);
+    } else {
+      const int t = 8 * wave + (lane >> 3);
+      set_m0(iss_dst + kRopeOff + wave_u * 1024);
+      lds_dma16<0>(iss_rope, rope_voff - (unsigned)(t - min(t, last)) * (kDr * 2));
+    }
+  };
   auto issue_part = [&](int i) {       // of a full tile (the instruction offset moves both sides)
+    if (MX4) return issue_part_mx4(i, kMTok - 1);
     if (i == 0 || i == 4) set_m0(iss_dst + wave_u * 8192 + i * 1024);
     if (i == 8) set_m0(iss_dst + kMLatBytes + wave_u * 1024);
     if (i == 8) lds_dma16<0>(iss_rope, rope_voff);
@@ -478,6 +515,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   };
   auto issue_part_any = [&](int i) {   // rows past the chunk's end re-read its last one (finite values, weight 0 later)
     const int last = min(kMTok, t1 - iss_tok) - 1;
+    if (MX4) return issue_part_mx4(i, last);
     if (i < 8) {
       const int t = 8 * wave_u + i;
       set_m0(iss_dst + t * 1024);
@@ -491,7 +529,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   auto issue_end = [&]() {
     iss_tok += kMTok;
     iss_slot += kMTok;
-    iss_dst = iss_dst == lds_base + (kPStages - 1) * kMStage ? lds_base : iss_dst + kMStage;
+    iss_dst = iss_dst == lds_base + (kPStages - 1) * kStageB ? lds_base : iss_dst + kStageB;
     if (iss_slot == p.page_size) {
       iss_slot = 0;
       ++iss_page_at;
@@ -515,7 +553,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   auto issue_whole = [&]() {
     issue_begin();
 #pragma unroll
-    for (int i = 0; i < kMLoads; ++i) issue_part_any(i);
+    for (int i = 0; i < kLoads; ++i) issue_part_any(i);
     issue_end();
   };
   // the first tile is requested behind the queries and waited for with them; they go into the accumulation file
@@ -528,13 +566,13 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   __builtin_amdgcn_sched_barrier(0);
   const int n_pro = min(ntiles, kPStages);
   for (int jj = 1; jj < n_pro; ++jj) issue_whole();
-  if (tid < 8) ((int*)(smem + kPFOff))[tid] = -1;
+  if (tid < 8) ((int*)(smem + kPF))[tid] = -1;
 
   // ---- per-lane LDS read offsets inside a stage (see mla_mfma_kernel; this wave's 16 tokens only)
   const int k_tok = c16 ^ ((c16 & 4) << 1);
   const int q4t = q4 ^ ((q4 & 1) << 1);
   const unsigned k_lat_off = (16 * th + k_tok) * 1024 + ((q4 ^ lat_swz(k_tok)) << 4);                     // ^ ((ks % 4) << 6), + 256 (ks / 4)
-  const unsigned k_rope_off = kMLatBytes + (16 * th + k_tok) * (kDr * 2) + ((q4 ^ rope_swz(k_tok)) << 4); // ^ (kr << 6)
+  const unsigned k_rope_off = kRopeOff + (16 * th + k_tok) * (kDr * 2) + ((q4 ^ rope_swz(k_tok)) << 4); // ^ (kr << 6)
   unsigned v_off;                                                             // ^ (mt << 6), + 16 KiB ss
   {
     const int k = (lane & 15) >> 2, seg = lane & 3, hb = (lane >> 4) & 1, ta = 4 * g + k;
@@ -561,8 +599,9 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   bf16x8 ka[18];
   short4v vlo[2][4], vhi[2][4];
   f32x4 s[2];
-  auto k_read = [&](unsigned base, int ks) {
-    const unsigned addr = ks < 16 ? ((base + k_lat_off) ^ ((ks & 3) << 6)) + (ks >> 2) * 256
+  // (base: the tile's stage; lat: where its latent channels are, the stage itself or the ring's tile)
+  auto k_read = [&](unsigned base, unsigned lat, int ks) {
+    const unsigned addr = ks < 16 ? ((lat + k_lat_off) ^ ((ks & 3) << 6)) + (ks >> 2) * 256
                                   : ((base + k_rope_off) ^ ((ks - 16) << 6));
     ka[ks] = *(lds_bf16x8_ptr)(size_t)addr;
   };
@@ -573,27 +612,52 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   };
   bf16x8 pb[2][2];
   auto p_read = [&](int par, int i) {           // i = 2 nt + ss
-    pb[i & 1][i >> 1] = *(const bf16x8*)(smem + kPPOff + par * kMPBytes + i * 1024 + lane * 16);
+    pb[i & 1][i >> 1] = *(const bf16x8*)(smem + kPP + par * kMPBytes + i * 1024 + lane * 16);
+  };
+  // (4 bits) unit u of a tile: row 8 wave + u, eight channels a lane
+  const unsigned wd_out[2] = {(unsigned)(lane * 16 ^ ((2 * wave) & 3) << 4), (unsigned)(lane * 16 ^ ((2 * wave + 1) & 3) << 4)};
+  unsigned wd_raw[8], wd_byte[8];
+  auto widen_read = [&](unsigned base, int u) {
+    typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
+    wd_raw[u] = *(u32_ptr)(size_t)(base + wave * (8 * kXRow) + u * kXRow + lane * 4);
+    wd_byte[u] = *(lds_byte_ptr)(size_t)(base + kXScales + wave * 256 + u * kXScaleRow + (lane >> 2));
+  };
+  auto widen_write = [&](unsigned lat, int u) {
+    typedef __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
+    *(u32x4_ptr)(size_t)(lat + (8 * wave + u) * 1024 + (wd_out[u >> 2] ^ ((u & 3) << 6))) =
+        mx4_tile::decode8(wd_raw[u], mx4_tile::scale_of(wd_byte[u]));
+  };
+  auto widen_tile = [&](unsigned base, unsigned lat) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < 8; ++u) widen_read(base, u);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) widen_write(lat, u);
   };
   // scores of a tile (its first operands already read), with the operands of the value product of the tile before it and, ISSUE, the
-  // second half of the loads of the tile after next
-  auto scores = [&](unsigned kb, unsigned vb, int par, auto with_v, auto issue, bool rest) {
+  // second half of the loads of the tile after next (4 bits: the tile in wd is widened into wl instead)
+  auto scores = [&](unsigned kb, unsigned kl, unsigned vb, int par, auto with_v, auto issue, bool rest, unsigned wd = 0u,
+                    unsigned wl = 0u) {
     constexpr bool ISSUE = decltype(issue)::value;
     s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 18; ++m) {
       s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[m], qreg[0][m], s[0], 0, 0, 0);
       s[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[m], qreg[1][m], s[1], 0, 0, 0);
-      if (m + kAhead < 18) k_read(kb, m + kAhead);
+      if (m + kAhead < 18) k_read(kb, kl, m + kAhead);
       if (decltype(with_v)::value && m < 16) v_read(vb, m);
       if (decltype(with_v)::value && m >= 10 && m < 14) p_read(par, m - 10);
-      if (m % 3 == 1 && m < 15) {
+      if (MX4 && decltype(with_v)::value) {
+        if (m < 8) widen_read(wd, m);
+        if (m >= 6 && m < 14) widen_write(wl, m - 6);
+      }
+      if (!MX4 && m % 3 == 1 && m < 15) {
         if (ISSUE) issue_part(4 + m / 3);
         else if (rest) issue_part_any(4 + m / 3);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (ISSUE || rest) issue_end();
+    if (!MX4 && (ISSUE || rest)) issue_end();
   };
   // the tile's maxima over this wave's 16 tokens, for the wave with the other 16 as well
   auto publish_max = [&](int par) {
@@ -604,7 +668,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     b = a;
     half_pairs(a, b);
     mx = fmaxf(a, b);
-    ((float*)(smem + kPXOff))[(par * 4 + wave) * 32 + c32] = mx;
+    ((float*)(smem + kPX))[(par * 4 + wave) * 32 + c32] = mx;
   };
   // The reference maxima (refreshed lazily, see decode_mfma.hip) from both halves' maxima; when one moves, its factor is
   // left for the waves that hold the head's history (both halves store the same).
@@ -620,8 +684,8 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
       l_run[0] *= a0;
       l_run[1] *= a1;
       both(-m_new, neg_m[0], neg_m[1]);
-      ((float*)(smem + kPAOff))[par * kMHeads + 32 * hg + c32] = alpha;
-      ((int*)(smem + kPFOff))[par * 4 + wave] = tile;
+      ((float*)(smem + kPA))[par * kMHeads + 32 * hg + c32] = alpha;
+      ((int*)(smem + kPF))[par * 4 + wave] = tile;
     }
   };
   float pe[2][4];
@@ -638,7 +702,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const bf16x4 pk = {(__bf16)pe[i][0], (__bf16)pe[i][1], (__bf16)pe[i][2], (__bf16)pe[i][3]};
-      *(bf16x4*)(smem + kPPOff + par * kMPBytes + i * 256 + p_wr_off) = pk;
+      *(bf16x4*)(smem + kPP + par * kMPBytes + i * 256 + p_wr_off) = pk;
     }
   };
   auto rescale = [&](int2 grown, int par, int tile) {      // a head's history loses weight when its maximum grew
@@ -646,7 +710,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     if (__builtin_expect(g0 == tile || g1 == tile, 0)) {
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) {
-        const float a_h = (nt == 0 ? g0 : g1) == tile ? ((const float*)(smem + kPAOff))[par * kMHeads + nt * 32 + c32] : 1.f;
+        const float a_h = (nt == 0 ? g0 : g1) == tile ? ((const float*)(smem + kPA))[par * kMHeads + nt * 32 + c32] : 1.f;
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
@@ -664,55 +728,75 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  auto partner_max = [&](int par) { return ((const float*)(smem + kPXOff))[(par * 4 + (wave ^ 2)) * 32 + c32]; };
-  auto grown_at = [&](int par) { return *(const int2*)(smem + kPFOff + par * 16); };   // waves 0, 1: heads 0..31, 32..63
-  auto after = [&](unsigned st) { return st == lds_base + (kPStages - 1) * kMStage ? lds_base : st + kMStage; };
+  auto partner_max = [&](int par) { return ((const float*)(smem + kPX))[(par * 4 + (wave ^ 2)) * 32 + c32]; };
+  auto grown_at = [&](int par) { return *(const int2*)(smem + kPF + par * 16); };   // waves 0, 1: heads 0..31, 32..63
+  auto after = [&](unsigned st) { return st == lds_base + (kPStages - 1) * kStageB ? lds_base : st + kStageB; };
+  const unsigned ring = lds_base + kXRing;
+  auto ring_after = [&](unsigned at) { return at == ring + 2 * kMLatBytes ? ring : at + kMLatBytes; };
 
   // ---- prologue: scores and probabilities of tile 0
-  if (ntiles > 3) wait_vm_lgkm<3 * kMLoads>();
-  else if (ntiles > 2) wait_vm_lgkm<2 * kMLoads>();
-  else if (ntiles > 1) wait_vm_lgkm<kMLoads>();
+  if (ntiles > 3) wait_vm_lgkm<3 * kLoads>();
+  else if (ntiles > 2) wait_vm_lgkm<2 * kLoads>();
+  else if (ntiles > 1) wait_vm_lgkm<kLoads>();
   else wait_vm_lgkm<0>();
+  if (MX4) {
+    widen_tile(lds_base, ring);
+    wait_vm_lgkm<63>();
+  }
   hand_over();
+  const unsigned lat0 = MX4 ? ring : lds_base, lat1 = MX4 ? ring + kMLatBytes : lds_base + kStageB;
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) k_read(lds_base, i);
-  scores(lds_base, 0u, 0, std::false_type{}, std::false_type{}, false);
+  for (int i = 0; i < kAhead; ++i) k_read(lds_base, lat0, i);
+  scores(lds_base, lat0, 0u, 0, std::false_type{}, std::false_type{}, false);
   publish_max(0);
-  if (ntiles > 3) wait_vm_lgkm<2 * kMLoads>();
-  else if (ntiles > 2) wait_vm_lgkm<kMLoads>();
+  if (ntiles > 3) wait_vm_lgkm<2 * kLoads>();
+  else if (ntiles > 2) wait_vm_lgkm<kLoads>();
   else wait_vm_lgkm<0>();
+  if (MX4) {
+    widen_tile(lds_base + kStageB, lat1);   // (one tile: whatever the stage holds, unused)
+    wait_vm_lgkm<63>();
+  }
   hand_over();                       // the maxima are visible, tile 1 has landed
+  if (MX4 && ntiles > kPStages) issue_whole();   // tile 4: the stage of tile 0 is free
   refresh(partner_max(0), 0, 0);
 #pragma unroll
   for (int e = 0; e < 4; ++e) soften(e, ntiles == 1 ? nvalid_last : kMTok);
   store_p(0);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) k_read(lds_base + kMStage, i);   // (one tile: whatever the stage holds, unused)
+  for (int i = 0; i < kAhead; ++i) k_read(lds_base + kStageB, lat1, i);   // (one tile: whatever the stage holds, unused)
 
   // ---- step j: scores of tile j + 1 while the operands of tile j's value product are read; one barrier; the value product
   // of tile j, with the softmax of tile j + 1 and the first operands of tile j + 2 between its MFMAs; one barrier, behind
   // which P^T of tile j + 1 is there.  The loads of tile j + 4 are spread over the second half of the step and the first
-  // half of the next.
+  // half of the next.  4 bits: the stage of tile j + 1 is free behind the first barrier, and takes tile j + 5 at once.
   bool rest = false;                 // the second half of a tile's loads is due
-  unsigned st_cur = lds_base;
+  unsigned st_cur = lds_base, ring_cur = ring;
   __builtin_amdgcn_sched_barrier(0);
   wait_lgkm<kAhead>();
   hand_over();                       // P^T of tile 0
   auto step = [&](auto issue, int j) {
-    constexpr bool ISSUE = decltype(issue)::value;         // tiles j + 3 and j + 4 exist and are no last ones
+    constexpr bool ISSUE = decltype(issue)::value;         // tiles j + 3 and j + 4 (4 bits: j + 5) exist and are no last ones
     const int par = j & 1, next = par ^ 1;
     const unsigned st_next = after(st_cur), st_then = after(st_next);
+    const unsigned ring_next = ring_after(ring_cur), ring_then = ring_after(ring_next);
+    const unsigned lat_cur = MX4 ? ring_cur : st_cur, lat_next = MX4 ? ring_next : st_next, lat_then = MX4 ? ring_then : st_then;
     __builtin_amdgcn_sched_barrier(0);
+    if (MX4) {                       // tile j + 2 has landed in this wave's share; j + 3 and j + 4 may be in flight
+      if (ISSUE || j + 4 < ntiles) wait_vmcnt<2 * kLoads>();
+      else wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+    }
     const int2 grown = grown_at(par);
-    scores(st_next, st_cur, par, std::true_type{}, issue, rest);
+    scores(st_next, lat_next, lat_cur, par, std::true_type{}, issue, rest, st_then, lat_then);
     publish_max(next);
     // tile j + 2 has landed in this wave's share, its reads of tile j are done, the maxima are stored
-    if (ISSUE || j + 3 < ntiles) wait_vm_lgkm<kMLoads>();
+    if (MX4) wait_vm_lgkm<63>();
+    else if (ISSUE || j + 3 < ntiles) wait_vm_lgkm<kLoads>();
     else wait_vm_lgkm<0>();
     hand_over();
     const float partner = partner_max(next);
-    rest = ISSUE || j + 4 < ntiles;
+    rest = ISSUE || j + (MX4 ? 5 : 4) < ntiles;
     const int valid = !ISSUE && j + 2 == ntiles ? nvalid_last : kMTok;
     rescale(grown, par, j);
     __builtin_amdgcn_sched_barrier(0);
@@ -728,26 +812,28 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
         else if (rest) issue_part_any(m >> 1);
       }
       if (m >= 3) {
-        k_read(st_then, 2 * (m - 3));
-        k_read(st_then, 2 * (m - 3) + 1);
+        k_read(st_then, lat_then, 2 * (m - 3));
+        k_read(st_then, lat_then, 2 * (m - 3) + 1);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    if (MX4 && (ISSUE || rest)) issue_end();
     wait_lgkm<4>();                  // (all but the last two pieces' reads: P^T is stored)
     hand_over();
     st_cur = st_next;
+    ring_cur = ring_next;
   };
   {
     int j = 0;
     if (ntiles > 1) step(std::false_type{}, j++);
-    for (; j + 5 < ntiles; ++j) step(std::true_type{}, j);
+    for (; j + (MX4 ? 6 : 5) < ntiles; ++j) step(std::true_type{}, j);
     for (; j + 1 < ntiles; ++j) step(std::false_type{}, j);
   }
   {
     const int j = ntiles - 1, par = j & 1;
     const int2 grown = grown_at(par);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v_read(st_cur, i);
+    for (int i = 0; i < 16; ++i) v_read(MX4 ? ring_cur : st_cur, i);
 #pragma unroll
     for (int i = 0; i < 4; ++i) p_read(par, i);
     rescale(grown, par, j);
@@ -774,7 +860,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
         }
     }
   }
-  float* const lbuf = (float*)(smem + kPXOff);       // (free since the barrier above)
+  float* const lbuf = (float*)(smem + kPX);       // (free since the barrier above)
 #pragma unroll
   for (int i = 0; i < 2; ++i) l_run[i] = head_sum(l_run[i]);
   if (th == 1 && lane < 32) lbuf[hg * 32 + lane] = lane < 16 ? l_run[0] : l_run[1];
@@ -809,6 +895,20 @@ static int launch_mla_as(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg
   return check_launch();
 }
 
+template <bool MX4>
+static int launch_mla_pipe(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) {
+  constexpr int lds = MX4 ? kXLds : kPLds;
+  static PerDeviceSetup setup;
+  int setup_dev = -1;
+  if (setup.needed(&setup_dev)) {
+    if (hipFuncSetAttribute((const void*)mla_pipe_kernel<MX4>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+      return MLRA_ERR_LAUNCH;
+    setup.done(setup_dev);
+  }
+  MLRA_LAUNCH_TIMED(a.t_main, mla_pipe_kernel<MX4>, dim3(n_wg), dim3(256), lds, a.stream, p);
+  return check_launch();
+}
+
 // The pipelined kernel has one workgroup per CU, 15 us of start-up and write-out each and 1.15 us per tile; the two-stage
 // kernel overlaps the start-up of one workgroup with another's tiles, 1.5 us each.  So the latter keeps launches of more
 // workgroups than CUs in short chunks, where these are not fitted (whole steps, two-stage against pipelined: 100 sequences of
@@ -827,6 +927,7 @@ int mla_mfma_stages(const DecodeArgs& a) {
 int launch_mla_mfma(const DecodeArgs& a) {
   MfmaParams p;
   p.latent = (const bf16_t*)a.latent;
+  p.scales = (const uint8_t*)a.scales;
   p.rope = (const bf16_t*)a.rope;
   p.page_table = a.page_table;
   p.seq_lens = a.seq_lens;
@@ -858,18 +959,11 @@ int launch_mla_mfma(const DecodeArgs& a) {
   if (!a.balanced && !a.fitted && (n_wg > a.cus || a.q_group > 1) && launch_seq_order(a) == MLRA_OK) p.seq_order = a.seq_order;
   // (the query tokens of one sequence are kept side by side in the order)
   p.split_major = p.seq_order && a.q_group <= 1;
+  if (a.scales) return launch_mla_pipe<true>(a, p, (unsigned)n_wg);
   const int stages = mla_mfma_stages(a);
   if (stages == 4) return launch_mla_as<4>(a, p, (unsigned)n_wg);
   if (stages == 2) return launch_mla_as<2>(a, p, (unsigned)n_wg);
-  static PerDeviceSetup setup;
-  int setup_dev = -1;
-  if (setup.needed(&setup_dev)) {
-    if (hipFuncSetAttribute((const void*)mla_pipe_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kPLds) != hipSuccess)
-      return MLRA_ERR_LAUNCH;
-    setup.done(setup_dev);
-  }
-  MLRA_LAUNCH_TIMED(a.t_main, mla_pipe_kernel, dim3((unsigned)n_wg), dim3(256), kPLds, a.stream, p);
-  return check_launch();
+  return launch_mla_pipe<false>(a, p, (unsigned)n_wg);
 }
 
 

@@ -160,9 +160,9 @@ struct Route {
 static Route choose_route(DecodeArgs& a) {
   Route r;
   r.kernel = decode_mfma_supported(a) ? kMlra
+             : mla_mfma_supported(a)  ? kMla
              : a.scales               ? kMx4
              : decode_gla_supported(a) ? kGla
-             : mla_mfma_supported(a)  ? kMla
              : decode_f32_supported(a) ? kF32
                                        : kPlain;
   r.merge_mfma = merge_upproj_mfma_supported(a);
@@ -382,7 +382,7 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   a.stream = (hipStream_t)stream;
   a.t_main = timing_pair(0);
   a.t_epi = timing_pair(1);
-  if (!decode_mfma_supported(a)) a.plan = plan_mx4(units, hb, c->n_blocks, max_seq_len, a.cus);
+  if (!decode_mfma_supported(a) && !mla_mfma_supported(a)) a.plan = plan_mx4(units, hb, c->n_blocks, max_seq_len, a.cus);
   int32_t* const lens = (int32_t*)workspace;
   int32_t* const table = (int32_t*)((char*)workspace + align_up((size_t)units * sizeof(int32_t), 256));
   carve_workspace(a, (char*)workspace + mx4_table_bytes(units, q_len, c->max_pages_per_seq));

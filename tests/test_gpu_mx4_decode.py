@@ -111,6 +111,29 @@ def test_long_contexts_in_chunks(dtype, lens, n_blocks, h):
     _check(lens, n_blocks=n_blocks, h=h, dtype=dtype, page=128)
 
 
+# whole sequences as one chunk each: the pipelined kernels at every distance from the end of their prologue, stages and ring,
+# last tiles full, of one token and of one short of full
+@pytest.mark.parametrize("n_blocks,h,groups,page", [(2, 128, 1, 64), (4, 64, 1, 16), (4, 128, 2, 32), (1, 130, 1, 128)])
+def test_tiles_of_the_pipelined_kernel(n_blocks, h, groups, page):
+    lens = [64 * t + e for t in range(1, 14) for e in (0, 1, 63)] + [0, 1, 2, 3]
+    lens += [5] * (260 // n_blocks)                       # (enough sequences for a chunk each)
+    _check(lens, n_blocks=n_blocks, h=h, groups=groups, page=page, d_h=32)
+
+
+@pytest.mark.parametrize("h,page", [(64, 32), (100, 64), (128, 96)])
+def test_tiles_of_the_mla_kernel(h, page):
+    lens = [32 * t + e for t in range(1, 12) for e in (0, 1, 31)] + [0, 1, 2, 700]
+    lens += [5] * 260
+    _check(lens, n_blocks=1, d_cb=512, h=h, page=page, d_h=32)
+
+
+@pytest.mark.parametrize("n_blocks,d_cb,h", [(1, 512, 128), (4, 128, 128), (4, 128, 64), (1, 128, 128)])
+def test_ragged_batches_in_chunks(n_blocks, d_cb, h):
+    rng = np.random.default_rng(4)
+    _check(rng.integers(0, 2500, size=20).tolist(), n_blocks=n_blocks, d_cb=d_cb, h=h, d_h=128)
+    _check([9000, 100, 6500], n_blocks=n_blocks, d_cb=d_cb, h=h, d_h=128, max_pages=400)
+
+
 def test_many_sequences():
     rng = np.random.default_rng(3)
     _check(rng.integers(0, 200, size=70).tolist(), n_blocks=2, h=64, d_h=32)
