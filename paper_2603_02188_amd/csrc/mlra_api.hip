@@ -292,6 +292,31 @@ static SplitPlan plan_mx4(int units, int h, int n_blocks, int max_seq_len, int c
   return plan_splits(units, n_blocks * ((h + 63) / 64), max_seq_len, 2 * cus);
 }
 
+// The pipelined kernels on a cache in 4 bits.  A workgroup has a compute unit to itself and costs about ten tiles beside its
+// own, so uniform chunks fill one round and never a little of a second one (24 sequences of 1K in two chunks 34 us, in three 50).
+// Long chunks of 4 to 64 sequences get slots for two rounds, and the decode kernel fits them to the lengths (chunk_fit.h).  That
+// pays for ragged batches and costs uniform ones the fit and a longer merge (whole steps, 128 heads, fitted against uniform:
+// MLRA-4 8 sequences of 4K to 32K 72 against 89 us, of 32K 102 against 97, 40 of 1K to 8K 98 against 131, 16 of 8K in chunks
+// of 2K 67 against 62; MLA, whose merge is the same, 64 of 1K to 8K 168 against 199, of 8K 221 against 214).  More than 16
+// sequences that fill the round as they are, and those that fill it uncut, are left alone (MLRA-2 64 of 8K 106, fitted 120,
+// of 1K to 8K 103 and 99; MLRA-4, whose partials are the merged rows then, 172 and 185, of 1K to 8K 152 and 132).
+static SplitPlan plan_mx4_fast(int units, int q_len, int h, int groups, int n_blocks, int d_cb, int max_seq_len, int cus) {
+  const bool mla = d_cb == 512, paired = !mla && decode_mfma_paired(h, n_blocks, groups);
+  const int per_unit = mla ? (h + 63) / 64 : paired ? n_blocks / 2 * ((h + 63) / 64) : n_blocks * ((h + 127) / 128);
+  const long wgs = (long)units * per_unit;
+  const int n_seqs = units / q_len;
+  if (n_seqs > 64 && wgs > cus / 2) return plan_decode(units, h, groups, n_blocks, d_cb, max_seq_len, cus);
+  const SplitPlan one = plan_splits(units, per_unit, max_seq_len, (int)std::max(cus - wgs + 1, 1L));   // floor(cus / wgs) chunks
+  const bool fills = !mla && 5 * wgs * one.n_splits > 4L * cus && (one.n_splits == 1 || n_seqs > 16);
+  if (n_seqs < 4 || n_seqs > 64 || one.chunk_tokens < (mla ? 1024 : 4096) || fills || (mla && q_len > 1)) return one;
+  SplitPlan two = plan_splits(units, per_unit, max_seq_len, 2 * cus);
+  // (no more slots than the bf16 epilogue takes)
+  const int bpg = n_blocks / groups, most = std::min(128 / bpg, (98176 - 64 * (bpg * d_cb + 8)) / (256 * bpg));
+  if (two.n_splits > most || two.n_splits <= one.n_splits) return one;
+  two.target_chunks = mla ? 0 : units;       // (fitted, see choose_route)
+  return two;
+}
+
 // (q_len > 1: a row of the lengths and of the page table per query in front of the partials)
 static size_t mx4_table_bytes(int units, int q_len, int max_pages) {
   return q_len == 1 ? 0 : align_up((size_t)units * sizeof(int32_t), 256) +
@@ -332,7 +357,7 @@ size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, 
   // (whichever kernel runs: that depends on the types and on d_r as well)
   return mx4_table_bytes(units, q_len, max_pages_per_seq) +
          std::max(decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4(units, hb, n_blocks, len, cus)),
-                  decode_ws_bytes(units, hb, n_blocks, d_cb, plan_decode(units, hb, groups, n_blocks, d_cb, len, cus)));
+                  decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4_fast(units, q_len, hb, groups, n_blocks, d_cb, len, cus)));
 }
 
 int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, int32_t h, int32_t d_h, int32_t groups,
@@ -353,7 +378,7 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 256 != 0) return MLRA_ERR_WORKSPACE;
   DecodeArgs a = {};
   a.cus = device_cu_count();
-  a.plan = plan_decode(units, hb, groups, c->n_blocks, c->d_cb, max_seq_len, a.cus);
+  a.plan = plan_mx4_fast(units, q_len, hb, groups, c->n_blocks, c->d_cb, max_seq_len, a.cus);
   a.latent = c->latent;
   a.scales = c->scales;
   a.rope = c->rope;

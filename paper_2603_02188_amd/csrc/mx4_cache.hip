@@ -59,8 +59,8 @@ __device__ __forceinline__ void store8(float* p, bool aligned, const u32x4& v) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(v[e] << 16); x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
   if (aligned) {
-    *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
-    *(f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, (f32x4*)p);
+    __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, (f32x4*)(p + 4));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = x[e];
@@ -68,35 +68,53 @@ __device__ __forceinline__ void store8(float* p, bool aligned, const u32x4& v) {
 }
 __device__ __forceinline__ void store8(bf16_t* p, bool aligned, const u32x4& v) {
   if (aligned) {
-    *(u32x4*)p = v;
+    __builtin_nontemporal_store(v, (u32x4*)p);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) { p[2 * e] = (bf16_t)v[e]; p[2 * e + 1] = (bf16_t)(v[e] >> 16); }
   }
 }
 
-// Calls fn(u, page, slot) for the tokens u < kTokensWave of this wave that exist and have a slot in the cache.
+// The tokens of a wave: where they lie is the same for all lanes.
 struct Tokens {
-  int first, count;        // first row of this wave, rows it has
   long long page[kTokensWave];
   int slot[kTokensWave];
-  bool ok[kTokensWave];
+  bool ok[kTokensWave];      // the row exists and has a slot in the cache
 };
 __device__ __forceinline__ Tokens tokens_of(const RowsParams& p, int s, int first) {
   Tokens t;
-  t.first = first;
   const int pos = p.positions[s], rows = p.row_lens ? min(p.row_lens[s], p.n_rows) : p.n_rows;
+  const long long at = (long long)pos + first;                     // slot of the first one in the sequence
+  const bool any = pos >= 0 && first < rows && at < (long long)p.max_pages * p.page_size;
+  unsigned index = any ? (unsigned)at / (unsigned)p.page_size : 0u, slot = any ? (unsigned)at % (unsigned)p.page_size : 0u;
 #pragma unroll
   for (int u = 0; u < kTokensWave; ++u) {
-    const long long at = (long long)pos + first + u;        // its slot in the sequence
-    const bool in = pos >= 0 && first + u < rows && at < (long long)p.max_pages * p.page_size;
-    const unsigned slot = in ? (unsigned)at : 0u;
-    const int page = in ? p.page_table[(size_t)s * p.max_pages + slot / (unsigned)p.page_size] : 0;
+    const bool in = any && first + u < rows && index < (unsigned)p.max_pages;
+    const int page = __builtin_amdgcn_readfirstlane(in ? p.page_table[(size_t)s * p.max_pages + index] : 0);
     t.ok[u] = in && (unsigned)page < (unsigned)p.num_pages;
     t.page[u] = page;
-    t.slot[u] = (int)(slot % (unsigned)p.page_size);
+    t.slot[u] = (int)slot;
+    if (++slot == (unsigned)p.page_size) {
+      slot = 0;
+      ++index;
+    }
   }
   return t;
+}
+
+// RoPE keys of the wave's tokens, one channel a lane: get and put take an element's index in the pool and in the rows (from
+// the wave's first one on).  All tokens' are in flight before the first is stored.
+template <typename Get, typename Put>
+__device__ __forceinline__ void each_rope(const RowsParams& p, const Tokens& t, Get get, Put put) {
+  for (int e = threadIdx.x & 63; e < p.d_r; e += 64) {
+    float x[kTokensWave];
+#pragma unroll
+    for (int u = 0; u < kTokensWave; ++u)
+      if (t.ok[u]) x[u] = get((size_t)(t.page[u] * p.page_size + t.slot[u]) * p.d_r + e, (size_t)u * p.d_r + e);
+#pragma unroll
+    for (int u = 0; u < kTokensWave; ++u)
+      if (t.ok[u]) put((size_t)(t.page[u] * p.page_size + t.slot[u]) * p.d_r + e, (size_t)u * p.d_r + e, x[u]);
+  }
 }
 
 // TS: type of the rows, TC: of the RoPE pool
@@ -105,11 +123,14 @@ __global__ __launch_bounds__(256) void mx4_append_kernel(RowsParams p, bool alig
   const int s = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int first = blockIdx.x * kTokensWG + wave * kTokensWave, d_c = p.n_blocks * p.d_cb;
   const Tokens t = tokens_of(p, s, first);
+  const long long planes = (long long)p.n_blocks * p.page_size;            // rows of all blocks of a page
   const size_t row0 = (size_t)s * p.n_rows + first;
   const TS* const src = (const TS*)p.c_kv + row0 * d_c;
   const TS* const k_src = (const TS*)p.k_rope + row0 * p.d_r;
   for (int c0 = 0; c0 < d_c; c0 += 512) {
     const int c = c0 + 8 * lane, cc = c < d_c ? c : 0, b = cc / p.d_cb, cb = cc - b * p.d_cb;
+    const size_t plane = (size_t)b * p.page_size, code_at = plane * (p.d_cb / 2) + cb / 2,
+                 scale_at = plane * (p.d_cb / kGroup) + cb / kGroup;       // of this lane, from row 0 of the page on
     float x[kTokensWave][8];
 #pragma unroll
     for (int u = 0; u < kTokensWave; ++u)
@@ -126,18 +147,13 @@ __global__ __launch_bounds__(256) void mx4_append_kernel(RowsParams p, bool alig
       const unsigned byte = scale_byte(top);
       const unsigned codes = byte == kNaNScale ? 0u : encode8(x[u], byte);
       if (c < d_c) {
-        const size_t row = ((size_t)t.page[u] * p.n_blocks + b) * p.page_size + t.slot[u];
-        *(unsigned*)(p.latent + row * (p.d_cb / 2) + cb / 2) = codes;
-        if ((lane & 3) == 0) p.scales[row * (p.d_cb / kGroup) + cb / kGroup] = (uint8_t)byte;
+        *(unsigned*)(p.latent + (t.page[u] * planes + t.slot[u]) * (p.d_cb / 2) + code_at) = codes;
+        if ((lane & 3) == 0) p.scales[(t.page[u] * planes + t.slot[u]) * (p.d_cb / kGroup) + scale_at] = (uint8_t)byte;
       }
     }
   }
-#pragma unroll
-  for (int u = 0; u < kTokensWave; ++u) {
-    if (!t.ok[u]) continue;
-    TC* const dst = (TC*)p.rope + ((size_t)t.page[u] * p.page_size + t.slot[u]) * p.d_r;
-    for (int e = lane; e < p.d_r; e += 64) store_f32(dst, e, load_f32(k_src, (size_t)u * p.d_r + e));
-  }
+  each_rope(p, t, [&](size_t, size_t own) { return load_f32(k_src, own); },
+            [&](size_t pool, size_t, float x) { store_f32((TC*)p.rope, pool, x); });
 }
 
 template <typename TS, typename TC>
@@ -145,29 +161,27 @@ __global__ __launch_bounds__(256) void mx4_read_kernel(RowsParams p, bool aligne
   const int s = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int first = blockIdx.x * kTokensWG + wave * kTokensWave, d_c = p.n_blocks * p.d_cb;
   const Tokens t = tokens_of(p, s, first);
+  const long long planes = (long long)p.n_blocks * p.page_size;            // rows of all blocks of a page
   const size_t row0 = (size_t)s * p.n_rows + first;
   TS* const dst = (TS*)p.c_kv + row0 * d_c;
   TS* const k_dst = (TS*)p.k_rope + row0 * p.d_r;
   for (int c0 = 0; c0 < d_c; c0 += 512) {
     const int c = c0 + 8 * lane, cc = c < d_c ? c : 0, b = cc / p.d_cb, cb = cc - b * p.d_cb;
+    const size_t plane = (size_t)b * p.page_size, code_at = plane * (p.d_cb / 2) + cb / 2,
+                 scale_at = plane * (p.d_cb / kGroup) + cb / kGroup;       // of this lane, from row 0 of the page on
     unsigned codes[kTokensWave], byte[kTokensWave];
 #pragma unroll
     for (int u = 0; u < kTokensWave; ++u)
       if (t.ok[u]) {
-        const size_t row = ((size_t)t.page[u] * p.n_blocks + b) * p.page_size + t.slot[u];
-        codes[u] = *(const unsigned*)(p.latent + row * (p.d_cb / 2) + cb / 2);
-        byte[u] = p.scales[row * (p.d_cb / kGroup) + cb / kGroup];
+        codes[u] = *(const unsigned*)(p.latent + (t.page[u] * planes + t.slot[u]) * (p.d_cb / 2) + code_at);
+        byte[u] = p.scales[(t.page[u] * planes + t.slot[u]) * (p.d_cb / kGroup) + scale_at];
       }
 #pragma unroll
     for (int u = 0; u < kTokensWave; ++u)
       if (t.ok[u] && c < d_c) store8(dst + (size_t)u * d_c + c, aligned, decode8(codes[u], scale_of(byte[u])));
   }
-#pragma unroll
-  for (int u = 0; u < kTokensWave; ++u) {
-    if (!t.ok[u]) continue;
-    const TC* const src = (const TC*)p.rope + ((size_t)t.page[u] * p.page_size + t.slot[u]) * p.d_r;
-    for (int e = lane; e < p.d_r; e += 64) store_f32(k_dst, (size_t)u * p.d_r + e, load_f32(src, e));
-  }
+  each_rope(p, t, [&](size_t pool, size_t) { return load_f32((const TC*)p.rope, pool); },
+            [&](size_t, size_t own, float x) { store_f32(k_dst, own, x); });
 }
 
 RowsParams rows_params(const mlra_mx4_cache* c, int n_rows, const int32_t* positions, const int32_t* row_lens,
