@@ -1210,14 +1210,15 @@ static bool want_seq_order(const DecodeArgs& a, long long n_wg) {
   return !a.balanced && !a.fitted && (n_wg > a.cus || a.q_group > 1);
 }
 
-// Pages of 16 or 32 tokens (a wave's 16 rows of a tile never straddle a page), or whole tiles.
+// Pages of 16 or 32 tokens (a wave's 16 rows of a tile never straddle a page), or whole tiles.  (4 bits: any multiple of 16.)
 static bool page_size_ok(int page_size) { return page_size == 16 || page_size == 32 || page_size % kTile == 0; }
 // (the kernels form page id x bytes-per-page from 32-bit factors)
 static bool page_bytes_ok(const DecodeArgs& a) { return (long long)a.n_blocks * a.page_size * a.d_cb * 2 < (1LL << 32); }
 
 bool decode_mfma_supported(const DecodeArgs& a) {
   // (the query rows are addressed with 32-bit byte offsets from q_abs / q_rope)
-  return a.dtype == MLRA_BF16 && a.d_cb == kDcb && a.d_r == kDr && page_size_ok(a.page_size) && page_bytes_ok(a) &&
+  return a.dtype == MLRA_BF16 && a.d_cb == kDcb && a.d_r == kDr &&
+         (a.scales ? a.page_size % 16 == 0 : page_size_ok(a.page_size)) && page_bytes_ok(a) &&
          a.plan.chunk_tokens % kTile == 0 &&
          (long long)a.batch * a.n_blocks * a.h * (kDcb * 2) < (1LL << 32) &&
          (long long)a.batch * a.h * a.groups * (kDr * 2) < (1LL << 32);

@@ -151,6 +151,14 @@ struct Route {
   bool planned;      // a kernel in front plans the chunks
 };
 
+// A cache in 4 bits on the pipelined kernels, where they take its shape: blocks of 128 channels, or one of 512.  Up to 32 heads
+// on a block without a neighbour leave three quarters of a workgroup idle, and the kernel for every shape is ahead (one block,
+// 32 heads, whole steps: 100 sequences of 8000 tokens 64 us against 87, 4 of 8192 26 against 30; 48 heads 80 and 88, 30 and 30,
+// 16 of 16K 44 and 42).
+static bool mx4_pipelined(const DecodeArgs& a) {
+  return (decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a);
+}
+
 // Which kernels a call takes, from its shape; sets a.fitted and a.fit_tiles.
 // Up to 64 sequences: the decode kernel finds its chunk from the lengths itself (chunk_fit.h), which saves the kernels in
 // front that would plan or order the chunks.  The MLRA kernel does so with long chunks and with several query tokens per
@@ -159,9 +167,9 @@ struct Route {
 // Other batches with a target: a kernel in front plans the chunks (both MFMA kernels read its table).
 static Route choose_route(DecodeArgs& a) {
   Route r;
-  r.kernel = decode_mfma_supported(a) ? kMlra
+  r.kernel = a.scales && !mx4_pipelined(a) ? kMx4
+             : decode_mfma_supported(a) ? kMlra
              : mla_mfma_supported(a)  ? kMla
-             : a.scales               ? kMx4
              : decode_gla_supported(a) ? kGla
              : decode_f32_supported(a) ? kF32
                                        : kPlain;
@@ -287,9 +295,11 @@ static int mx4_rows_common(const mlra_mx4_cache* c, int batch, int n_rows, const
   return check_mx4_cache(c, batch);
 }
 
-// The kernel for every shape runs two workgroups at a time on a compute unit, one per 64 heads at most.
-static SplitPlan plan_mx4(int units, int h, int n_blocks, int max_seq_len, int cus) {
-  return plan_splits(units, n_blocks * ((h + 63) / 64), max_seq_len, 2 * cus);
+// The kernel for every shape: as many chunks as its workgroups that run at a time.
+static SplitPlan plan_mx4(int units, int h, int n_blocks, int d_cb, int dtype, int max_seq_len, int cus) {
+  const int heads = mx4_heads_per_wg(h, d_cb, dtype), per_unit = n_blocks * ((h + heads - 1) / heads);
+  const long wgs = (long)units * per_unit, at_once = (long)cus * mx4_resident(heads, d_cb, dtype);
+  return plan_splits(units, per_unit, max_seq_len, (int)std::max(at_once - wgs + 1, 1L));
 }
 
 // The pipelined kernels on a cache in 4 bits.  A workgroup has a compute unit to itself and costs about ten tiles beside its
@@ -356,8 +366,9 @@ size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, 
   const int units = batch * q_len, hb = h / groups, len = max_pages_per_seq * page_size, cus = device_cu_count();
   // (whichever kernel runs: that depends on the types and on d_r as well)
   return mx4_table_bytes(units, q_len, max_pages_per_seq) +
-         std::max(decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4(units, hb, n_blocks, len, cus)),
-                  decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4_fast(units, q_len, hb, groups, n_blocks, d_cb, len, cus)));
+         std::max({decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4(units, hb, n_blocks, d_cb, MLRA_BF16, len, cus)),
+                  decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4(units, hb, n_blocks, d_cb, MLRA_F32, len, cus)),
+                  decode_ws_bytes(units, hb, n_blocks, d_cb, plan_mx4_fast(units, q_len, hb, groups, n_blocks, d_cb, len, cus))});
 }
 
 int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, int32_t h, int32_t d_h, int32_t groups,
@@ -407,7 +418,7 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   a.stream = (hipStream_t)stream;
   a.t_main = timing_pair(0);
   a.t_epi = timing_pair(1);
-  if (!decode_mfma_supported(a) && !mla_mfma_supported(a)) a.plan = plan_mx4(units, hb, c->n_blocks, max_seq_len, a.cus);
+  if (!mx4_pipelined(a)) a.plan = plan_mx4(units, hb, c->n_blocks, c->d_cb, c->dtype, max_seq_len, a.cus);
   int32_t* const lens = (int32_t*)workspace;
   int32_t* const table = (int32_t*)((char*)workspace + align_up((size_t)units * sizeof(int32_t), 256));
   carve_workspace(a, (char*)workspace + mx4_table_bytes(units, q_len, c->max_pages_per_seq));

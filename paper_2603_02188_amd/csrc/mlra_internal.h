@@ -188,7 +188,8 @@ int launch_mx4_append(const mlra_mx4_cache* c, int batch, int n_rows, const void
 int launch_mx4_read(const mlra_mx4_cache* c, int batch, int n_rows, const int32_t* positions, const int32_t* row_lens,
                     void* c_kv, void* k_rope, int dst_dtype, hipStream_t stream);
 constexpr int kMx4MaxBlock = 512, kMx4MaxRope = 128;   // channels that the decode kernel takes
-int mx4_heads_per_wg(int h, int d_cb, int dtype);
+int mx4_heads_per_wg(int h, int d_cb, int dtype);      // of the kernel for every shape
+int mx4_resident(int heads, int d_cb, int dtype);      // its workgroups that a compute unit runs at a time
 int launch_mx4_decode(const DecodeArgs& a);
 
 // ---- pre-attention of the new token (pre_attn.hip) ----------------------------------------------

@@ -430,8 +430,8 @@ int launch_one(const DecodeArgs& a, Mx4Params& p) {
 
 template <typename T, int DP, int RP, bool VEC>
 int launch_heads(const DecodeArgs& a, Mx4Params& p) {
-  if constexpr (DP > 256 || (DP > 128 && Terms<T>::n > 1)) {
-    return launch_one<T, DP, RP, 1, VEC>(a, p);      // (queries and accumulators of 32 heads do not fit a lane's registers)
+  if constexpr (DP > 256 || (DP > 64 && Terms<T>::n > 1)) {
+    return launch_one<T, DP, RP, 1, VEC>(a, p);
   } else {
     return mx4_heads_per_wg(a.h, a.d_cb, a.dtype) == 64 ? launch_one<T, DP, RP, 2, VEC>(a, p)
                                                         : launch_one<T, DP, RP, 1, VEC>(a, p);
@@ -450,8 +450,16 @@ int launch_typed(const DecodeArgs& a, Mx4Params& p) {
 
 }  // namespace
 
+// Heads per workgroup: 64 share a tile's trip through LDS where the queries and accumulators of 32 heads leave a lane's
+// registers room for a second wave on the SIMD.
 int mx4_heads_per_wg(int h, int d_cb, int dtype) {
-  return h > 32 && d_cb <= (dtype == MLRA_BF16 ? 256 : 128) ? 64 : 32;
+  return h > 32 && d_cb <= (dtype == MLRA_BF16 ? 256 : 64) ? 64 : 32;
+}
+
+// (More than two fit for narrow blocks, but their chunks cost the merge more than they save: 8 sequences of 1000 to 4000 tokens
+// x 16 heads x 4 blocks of 64 channels 30 us in 512 workgroups, 36 in 1024.)
+int mx4_resident(int heads, int d_cb, int dtype) {
+  return d_cb <= (dtype == MLRA_BF16 ? (heads == 32 ? 256 : 128) : 128) ? 2 : 1;
 }
 
 int launch_mx4_decode(const DecodeArgs& a) {

@@ -67,7 +67,7 @@ def _check(lens, n_blocks=4, d_cb=128, d_r=64, h=128, d_h=128, groups=1, q_len=1
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("page", [64, 16, 1, 7, 48, 256])
+@pytest.mark.parametrize("page", [64, 16, 1, 7, 48, 80, 256])
 def test_lengths_and_pages(dtype, page):
     _check([0, 1, 2, 63, 64, 65, 129, 300], page=page, dtype=dtype, h=32, n_blocks=2, d_h=32)
 
@@ -113,7 +113,7 @@ def test_long_contexts_in_chunks(dtype, lens, n_blocks, h):
 
 # whole sequences as one chunk each: the pipelined kernels at every distance from the end of their prologue, stages and ring,
 # last tiles full, of one token and of one short of full
-@pytest.mark.parametrize("n_blocks,h,groups,page", [(2, 128, 1, 64), (4, 64, 1, 16), (4, 128, 2, 32), (1, 130, 1, 128)])
+@pytest.mark.parametrize("n_blocks,h,groups,page", [(2, 128, 1, 64), (4, 64, 1, 16), (4, 128, 2, 32), (1, 130, 1, 128), (1, 70, 1, 48), (2, 64, 1, 112)])
 def test_tiles_of_the_pipelined_kernel(n_blocks, h, groups, page):
     lens = [64 * t + e for t in range(1, 14) for e in (0, 1, 63)] + [0, 1, 2, 3]
     lens += [5] * (260 // n_blocks)                       # (enough sequences for a chunk each)
