@@ -482,25 +482,24 @@ class Mx4Cache:
                    torch.empty((num_pages, page_size, d_r), dtype=dtype, device=dev), page_table, seq_lens)
 
     def struct(self) -> _Mx4CacheStruct:
-        P, NB, ps, half = self.latent.shape
-        assert self.latent.dtype == torch.uint8 and self.scales.dtype == torch.uint8
-        assert self.scales.shape == (P, NB, ps, half // 16) and half % 16 == 0
-        assert self.rope.shape[:2] == (P, ps) and self.rope.dim() == 3
-        assert self.page_table.dtype == torch.int32 and self.seq_lens.dtype == torch.int32
-        return _Mx4CacheStruct(_ptr(self.latent), _ptr(self.scales), _ptr(self.rope), _ptr(self.page_table),
-                               _ptr(self.seq_lens), P, ps, self.page_table.shape[1], NB, 2 * half, self.rope.shape[2],
-                               _dt(self.rope.dtype))
+        latent, scales, rope, table, lens = self.latent, self.scales, self.rope, self.page_table, self.seq_lens
+        P, NB, ps, half = latent.shape
+        rope_pages, rope_slots, d_r = rope.shape
+        assert latent.dtype == scales.dtype == torch.uint8 and table.dtype == lens.dtype == torch.int32
+        assert half % 16 == 0 and scales.shape == (P, NB, ps, half // 16) and rope_pages == P and rope_slots == ps
+        return _Mx4CacheStruct(_ptr(latent), _ptr(scales), _ptr(rope), _ptr(table), _ptr(lens), P, ps, table.shape[1], NB,
+                               2 * half, d_r, _dt(rope.dtype))
 
     @property
     def max_seq_len(self) -> int:
         return int(self.page_table.shape[1] * self.latent.shape[2])
 
 
-def _mx4_rows(cs: _Mx4CacheStruct, c_kv, k_rope, positions, row_lens):
+def _mx4_rows(cache: Mx4Cache, cs: _Mx4CacheStruct, c_kv, k_rope, positions, row_lens):
     batch, n_rows, d_c = c_kv.shape
     assert d_c == cs.n_blocks * cs.d_cb and k_rope.shape == (batch, n_rows, cs.d_r) and c_kv.dtype == k_rope.dtype
-    for t in (positions, row_lens):
-        assert t is None or (t.dtype == torch.int32 and t.shape == (batch,))
+    assert cache.page_table.shape[0] == batch and positions.dtype == torch.int32 and positions.shape == (batch,)
+    assert row_lens is None or (row_lens.dtype == torch.int32 and row_lens.shape == (batch,))
     return batch, n_rows
 
 
@@ -509,8 +508,7 @@ def mlra_mx4_append_kv(cache: Mx4Cache, c_kv: torch.Tensor, k_rope: torch.Tensor
     """Quantises rows c_kv [batch][n_rows][n_blocks*d_cb], k_rope [batch][n_rows][d_r] into slots positions[s] + j,
     j < new_lens[s] (n_rows if not given)."""
     cs = cache.struct()
-    batch, n_rows = _mx4_rows(cs, c_kv, k_rope, positions, new_lens)
-    assert cache.page_table.shape[0] == batch
+    batch, n_rows = _mx4_rows(cache, cs, c_kv, k_rope, positions, new_lens)
     _check(load_library().mlra_mx4_append_kv(ctypes.byref(cs), batch, n_rows, _ptr(c_kv), _ptr(k_rope), _dt(c_kv.dtype),
                                              _ptr(positions), _ptr(new_lens), _stream(stream)), "mlra_mx4_append_kv")
 
@@ -520,8 +518,7 @@ def mlra_mx4_read_kv(cache: Mx4Cache, positions: torch.Tensor, row_lens: Optiona
     """Slots positions[s] + j, j < row_lens[s] (all rows of the outputs if None), into row j of c_kv_out
     [batch][n_rows][n_blocks*d_cb] and k_rope_out [batch][n_rows][d_r]; the rows behind them are left as they were."""
     cs = cache.struct()
-    batch, n_rows = _mx4_rows(cs, c_kv_out, k_rope_out, positions, row_lens)
-    assert cache.page_table.shape[0] == batch
+    batch, n_rows = _mx4_rows(cache, cs, c_kv_out, k_rope_out, positions, row_lens)
     _check(load_library().mlra_mx4_read_kv(ctypes.byref(cs), batch, n_rows, _ptr(positions), _ptr(row_lens), _ptr(c_kv_out),
                                            _ptr(k_rope_out), _dt(c_kv_out.dtype), _stream(stream)), "mlra_mx4_read_kv")
     return c_kv_out, k_rope_out
@@ -541,10 +538,10 @@ def mlra_mx4_decode_attn(cache: Mx4Cache, q_abs: torch.Tensor, q_rope: torch.Ten
     """q_abs [batch][q_len][n_blocks][h / groups][d_cb], q_rope [batch][q_len][h][d_r] -> out [batch][q_len][h][d_h]; without
     the q_len dimension (one query token) in all of them, out has none either."""
     cs = cache.struct()
-    single = q_abs.dim() == 4
-    lead = tuple(q_abs.shape[:1]) if single else tuple(q_abs.shape[:2])
-    n_blocks, hb, d_cb = q_abs.shape[-3:]
-    batch, q_len, h, d_h = lead[0], 1 if single else lead[1], hb * groups, w_uv.shape[2] // hb
+    *lead, n_blocks, hb, d_cb = q_abs.shape
+    assert len(lead) in (1, 2)
+    batch, q_len, h, d_h = lead[0], lead[1] if len(lead) == 2 else 1, hb * groups, w_uv.shape[2] // hb
+    lead = tuple(lead)
     assert (n_blocks, d_cb) == (cs.n_blocks, cs.d_cb) and w_uv.shape == (n_blocks, d_cb, hb * d_h)
     assert q_rope.shape == lead + (h, cs.d_r) and cache.page_table.shape[0] == batch and cache.seq_lens.shape == (batch,)
     for t in (q_abs, q_rope, w_uv) + (() if gate is None else (gate,)):
