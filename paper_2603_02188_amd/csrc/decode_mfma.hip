@@ -33,9 +33,12 @@
 // 32 KiB exchange buffer; two workgroup barriers per tile.
 //
 // MX4, for the latent cache in 4 bits (plain and PAIRED form): the stages hold the codes and scales as they lie in memory
-// (13 or 17 KiB) and a ring of three tiles holds the latent channels widened to bf16, which is exact.  Each wave widens the
-// 16 rows that it has loaded itself, tile j + 2 during the scores of step j, so that the wait for its own loads is enough;
-// the step's barrier hands the rows to the others.
+// (13 or 17 KiB).  The scores take them as they are: v_mfma_scale_f32_32x32x64_f8f6f4 multiplies E2M1 codes, scaled by group,
+// with E2M3 numbers at four times the rate of bf16, and a query is the sum of two of those (see the prologue), so that the
+// latent channels cost half of what they do in bf16.  The RoPE channels stay bf16.  For the values, whose scales run along the
+// wrong axis for that instruction (a scale per token, which is the k index there), two tiles are widened to bf16, which is
+// exact: each wave widens the 16 rows that it loaded itself, tile j + 2 behind the value MFMAs of step j, into the place of
+// tile j.
 #include "chunk_fit.h"
 #include "mfma_tile.h"
 #include "mx4_tile.h"
@@ -240,6 +243,13 @@ __device__ __forceinline__ f32x4 acc_read4() {
   return f32x4{acc_read<base>(), acc_read<base + 1>(), acc_read<base + 2>(), acc_read<base + 3>()};
 }
 
+// The bf16 ring of the MX4 forms: two tiles, and room for the queries (48 KiB, or 40 KiB) before the first.
+constexpr int mx4_ring_bytes(int blocks) { return blocks == 1 ? 3 * kLatBytes : 4 * kLatBytes; }
+typedef __attribute__((ext_vector_type(6))) unsigned u32x6;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
+typedef __attribute__((ext_vector_type(32))) float f32x32;
+
 // What a workgroup costs beside its tiles (start-up, write-out), in tiles of about 1.1 us: sections of its life in the
 // 16-tile launch of 16 sequences of 16K tokens.
 constexpr int kFitOverhead = 10;
@@ -257,7 +267,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   constexpr int kStageB = kRopeOff + kRopeBytes;            // 24 KiB, or 40 KiB (MX4: 13 or 17)
   constexpr int kLoadsTile = MX4 ? kBlocksWG + 3 : 4 * kBlocksWG + 2;   // direct-to-LDS loads per wave and tile
   constexpr int kRingTile = MX4 ? kBlocksWG * kLatBytes : 0;   // (MX4) one tile of the bf16 ring, in front of the stages
-  constexpr int kRing = 3 * kRingTile;
+  constexpr int kRing = MX4 ? mx4_ring_bytes(kBlocksWG) : 0;
   constexpr int kHeadsPerWG = PAIRED ? 64 : kHeadsWG;
   // Workgroup -> (sequence, chunk, block, head group).  The workgroups of one (sequence, chunk) read the
   // same RoPE rows (and, across head groups, the same latent rows).  Workgroup ids go round-robin over
@@ -406,9 +416,11 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   const size_t lat_plane_bytes = (size_t)p.page_size * kRowB;          // one block's rows inside a page
   const size_t lat_half_step = GLA ? kDcb * 2 : lat_plane_bytes;       // from the first latent tile's source to the second's
   const char* lat_blk = (const char*)p.latent + (size_t)blk0 * lat_plane_bytes;
-  // (MX4: a lane loads 16 bytes of codes, row lane / 4, and the four scales of row lane % 16, PAIRED lanes 16 .. 31 those of
+  // (MX4: a lane loads 16 bytes of codes, row t = lane / 4, group (lane % 4) ^ (t / 4) % 4 (the LDS reads of one group of sixteen
+  // rows then hit sixteen different bank groups), and the four scales of row lane % 16, PAIRED lanes 16 .. 31 those of
   // the second block)
   constexpr int kScaleRow = kDcb / mx4_tile::kGroup;
+  const unsigned raw_piece = ((lane & 3) ^ ((lane >> 4) & 3)) << 4;
   const unsigned sc_page_bytes = (unsigned)p.n_blocks * (unsigned)p.page_size * (unsigned)kScaleRow;
   const unsigned sc_plane = PAIRED ? ((lane >> 4) & 1) * (unsigned)p.page_size * (unsigned)kScaleRow : 0u;
   const char* sc_blk = (const char*)p.scales + (size_t)blk0 * p.page_size * kScaleRow;
@@ -435,7 +447,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     if (MX4 && part <= kBlocksWG) {
       if (part < kBlocksWG) {
         set_m0(iss_stage + part * kRawBytes + wave_u * 1024);
-        lds_dma16<0>(iss_lat + part * lat_plane_bytes, lane * 16);
+        lds_dma16<0>(iss_lat + part * lat_plane_bytes, (lane >> 2) * kRowB + raw_piece);
       } else {
         set_m0(iss_stage + kBlocksWG * kRawBytes + wave_u * 256);
         lds_dma4(iss_sc, (lane & 15) * kScaleRow + sc_plane);
@@ -490,7 +502,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 #pragma unroll
       for (int jb = 0; jb < kBlocksWG; ++jb) {
         set_m0(stage + jb * kRawBytes + wave_u * 1024);
-        lds_dma16<0>(src_lat + jb * lat_half_step, (unsigned)(min(w0 + (lane >> 2), last) - first) * kRowB + (lane & 3) * 16);
+        lds_dma16<0>(src_lat + jb * lat_half_step, (unsigned)(min(w0 + (lane >> 2), last) - first) * kRowB + raw_piece);
       }
       set_m0(stage + kBlocksWG * kRawBytes + wave_u * 256);
       lds_dma4(sc_blk + (unsigned long long)page * sc_page_bytes + (unsigned)slot * (unsigned)kScaleRow,
@@ -565,6 +577,24 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 #pragma unroll
     for (int ks = 0; ks < 12; ++ks) load_k_part(st_off, lat_off, ks, ka);
   };
+  // (MX4) K operands as they are cached: 64 channels of a token are 16 bytes a lane and a scale byte, which the matrix
+  // instruction applies itself; byte 2 ks of ksc is the scale of operand ks
+  mx4_tile::u32x4 kraw[2];
+  unsigned ksc = 0;
+  const unsigned kx_off = (PAIRED ? hw * kRawBytes : 0) + s_tok * kRowB + ((g ^ ((s_tok >> 2) & 3)) << 4);
+  const unsigned kx_sc = kBlocksWG * kRawBytes + (s_tok >> 4) * 256 + (PAIRED ? hw * 64 : 0) + (s_tok & 15) * kScaleRow;
+  auto load_kx_part = [&](unsigned st_off, int part, bf16x8 (&ka)[12]) {   // 0, 1: codes; 2: scales; 3 .. 6: RoPE
+    typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
+    typedef const __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
+    if (part < 2) kraw[part] = *(u32x4_ptr)(size_t)((stage_base + st_off + kx_off) ^ (part << 5));
+    else if (part == 2) ksc = *(u32_ptr)(size_t)(stage_base + st_off + kx_sc);
+    else load_k_part(st_off, 0u, 5 + part, ka);
+  };
+  auto load_kx = [&](unsigned st_off, bf16x8 (&ka)[12]) {
+#pragma unroll
+    for (int part = 0; part < 7; ++part) load_kx_part(st_off, part, ka);
+    ksc >>= 8 * g;
+  };
   // transposed V operand (32 channels of tile mt x 16 of this wave's token rows) of the tile in that stage
   auto load_v_part = [&](unsigned st_off, int ss, int mt, bf16x8 (&va)[2][4]) {
     const unsigned lo_base = lds_base + st_off + v_off[0];
@@ -587,7 +617,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   auto widen_read = [&](unsigned st_off, int u) {
     typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
     const int jb = u >> 2, i = u & 3;
-    cv_raw[u] = *(u32_ptr)(size_t)(stage_base + st_off + cv_codes + jb * kRawBytes + i * 256);
+    cv_raw[u] = *(u32_ptr)(size_t)(((stage_base + st_off + cv_codes) ^ (i << 4)) + jb * kRawBytes + i * 256);
     cv_byte[u] = *(lds_byte_ptr)(size_t)(stage_base + st_off + cv_scale + jb * 64 + i * 16);
   };
   auto widen_half = [&](int u, int half) {       // four of the eight channels
@@ -663,6 +693,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   }
   acc_zero(pb0[1]);
   auto hold = [&](const bf16x8& x) { asm volatile("" : : "v"(x)); };
+  auto hold_raw = [&](const mx4_tile::u32x4& x) { asm volatile("" : : "v"(x)); };
   auto settle_acc = [&]() {   // (the operands of the last PV MFMAs stay put meanwhile)
     asm volatile("s_nop 15\n\ts_nop 15" : : "v"(va[1][2]), "v"(va[1][3]), "v"(pb0[1]), "v"(pb1[1]) : MLRA_ACC_CLOBBERS);
   };
@@ -727,6 +758,23 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   auto score_first = [&](f32x16& acc, const bf16x8& kt, const bf16x8& qt, const f32x16& init) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(acc) : "v"(kt), "a"(qt), "v"(init));
   };
+  // (MX4) S^T += K Q^T for 64 channels: E2M1 codes with their scales against one of the two E2M3 terms of a query
+  auto score_mx = [&](f32x16& acc, int ks, int term, const u32x6& qt, unsigned qsc) {
+    switch (2 * ks + term) {
+      case 0: asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:2"
+                           : "+v"(acc) : "v"(kraw[0]), "a"(qt), "v"(ksc), "v"(qsc)); break;
+      case 1: asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:2"
+                           : "+v"(acc) : "v"(kraw[0]), "a"(qt), "v"(ksc), "v"(qsc)); break;
+      case 2: asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:2"
+                           : "+v"(acc) : "v"(kraw[1]), "a"(qt), "v"(ksc), "v"(qsc)); break;
+      default: asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,1,0] op_sel_hi:[1,1,0] cbsz:4 blgp:2"
+                            : "+v"(acc) : "v"(kraw[1]), "a"(qt), "v"(ksc), "v"(qsc)); break;
+    }
+  };
+  auto score_mx_first = [&](f32x16& acc, const u32x6& qt, unsigned qsc, const f32x16& init) {
+    asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %3, %4, %5 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:2"
+                 : "=&v"(acc) : "v"(kraw[0]), "a"(qt), "v"(init), "v"(ksc), "v"(qsc));
+  };
   auto prob_pack = [&](int r, float p0, float p1, bf16x8 (&pb)[2]) {
     bf16x2 pp = {(__bf16)p0, (__bf16)p1};
     asm volatile("" : "+v"(pp));
@@ -743,6 +791,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 
   // ---- prologue: every stage gets a tile; scores and column maxima of tile 0; K operands of tile 1 ----
   bf16x8 qreg[2][12];
+  u32x6 qmx[2][2][2];           // (MX4) [head tile][64 channels][term]
+  unsigned qmx_sc[2] = {0, 0};  // ... and their scales, byte 2 ks + term
   issue_last_tile();
   for (int jj = 1; jj < STAGES - kQStages && jj < ntiles; ++jj) issue_tile();
   if (GLA && tid < 4) ((float*)(smem + STAGES * kStageB))[tid] = 0.f;   // the zeros some RoPE reads below take
@@ -767,17 +817,53 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       // the RoPE term is counted once; the other wave's channels are read from 16 bytes of zeros
       qaddr[8 + ks] = (!GLA || (ks >> 1) == hw) ? addr : lds_base + STAGES * kStageB;
     }
+    if (MX4) {
+      // A lane's 32 channels of operand ks are one group of the other side, channels 64 ks + 32 g .. + 31: a query there is
+      // hi + lo, E2M3 numbers (four significant bits, up to 7.5) with a power of two each, 2^-5 apart.  What is left is
+      // 2^-10 of the group's largest channel at most, less than a query in bf16 is off in the mean (0.11 % against 0.165 %).
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x32 x;
+        unsigned top = 0;
+        f32x32 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bf16x8 part = *(lds_bf16x8_ptr)(size_t)(q_lds + row * (kDcb * 2) + (((8 * ks + 4 * g + i) ^ (row & 15)) << 4));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[8 * i + e] = (float)part[e] * sc;
+            top = max(top, __float_as_uint(v[8 * i + e]) & 0x7fffffffu);
+          }
+        }
+        // (7.5 is the largest: from 1.875 2^e on the next power of two; a group with an infinity or a NaN is NaN)
+        const int ex = min(max((int)((top + 0x100000u) >> 23) - 2, 7), 252);
+        const bool finite = top < 0x7f800000u;
+        const float s_hi = __uint_as_float((unsigned)ex << 23), s_lo = __uint_as_float((unsigned)(ex - 5) << 23);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = (__bf16)v[e];
+        u32x6 hi = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, s_hi);
+        const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(hi, s_hi);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = (__bf16)(v[e] - back[e]);
+        u32x6 lo = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, s_lo);
+        qmx_sc[nt] |= (finite ? (unsigned)ex | (unsigned)(ex - 5) << 8 : 0xffffu) << (16 * ks);
+        asm volatile("" : "+a"(hi), "+a"(lo));
+        qmx[nt][ks][0] = hi;
+        qmx[nt][ks][1] = lo;
+      }
+    }
+    constexpr int kFirst = MX4 ? 8 : 0;
     bf16x8 raw[12];
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks) raw[ks] = *(lds_bf16x8_ptr)(size_t)qaddr[ks];
+    for (int ks = kFirst; ks < 12; ++ks) raw[ks] = *(lds_bf16x8_ptr)(size_t)qaddr[ks];
     if (!q_ready) {
 #pragma unroll
-      for (int ks = 0; ks < 12; ++ks)
+      for (int ks = kFirst; ks < 12; ++ks)
 #pragma unroll
         for (int e = 0; e < 8; ++e) raw[ks][e] = (__bf16)((float)raw[ks][e] * sc);
     }
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks) {
+    for (int ks = kFirst; ks < 12; ++ks) {
       asm volatile("" : "+a"(raw[ks]));   // into the accumulation file, where the score MFMAs read it
       qreg[nt][ks] = raw[ks];
     }
@@ -797,14 +883,31 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   f32x16 sa0, sa1, sb0, sb1;
   bf16x8 ka[12];
   {
-    load_k(0, 0, ka);
+    if (MX4) load_kx(0, ka);
+    else load_k(0, 0, ka);
 #pragma unroll
     for (int i = 0; i < 16; ++i) { sa0[i] = 0.f; sa1[i] = 0.f; }
+    if (MX4) {
 #pragma unroll
-    for (int ks = 0; ks < 12; ++ks) {
+      for (int ks = 0; ks < 2; ++ks) {
+        const i32x8 kt = {(int)kraw[ks][0], (int)kraw[ks][1], (int)kraw[ks][2], (int)kraw[ks][3], 0, 0, 0, 0};
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int term = 0; term < 2; ++term) {
+            const u32x6 q = qmx[nt][ks][term];
+            const i32x8 qt = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0};
+            f32x16& acc = nt == 0 ? sa0 : sa1;
+            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kt, qt, acc, 4, 2, 0, ksc >> (16 * ks), 0,
+                                                                  qmx_sc[nt] >> (16 * ks + 8 * term));
+          }
+      }
+    }
+#pragma unroll
+    for (int ks = MX4 ? 8 : 0; ks < 12; ++ks) {
       sa0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qreg[0][ks], sa0, 0, 0, 0);
       sa1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qreg[1][ks], sa1, 0, 0, 0);
-      if (ks == 1) asm volatile("" : : "v"(ka[0]));   // see the main loop
+      if (!MX4 && ks == 1) asm volatile("" : : "v"(ka[0]));   // see the main loop
     }
     // the maxima read the accumulators through asm, which the compiler's MFMA hazard bookkeeping does
     // not see: let the last score MFMA retire first
@@ -842,7 +945,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     // exists); their probabilities are what has to vanish.
     if (nvalid_last < kTile) { mask_tail(sa0); mask_tail(sa1); }
     __builtin_amdgcn_sched_barrier(0);
-    load_k((1 % STAGES) * kStageB, MX4 ? kRingTile : (1 % STAGES) * kStageB, ka);   // (a stale stage if the chunk has a single tile: those scores are never used)
+    if (MX4) load_kx((1 % STAGES) * kStageB, ka);
+    else load_k((1 % STAGES) * kStageB, (1 % STAGES) * kStageB, ka);   // (a stale stage if the chunk has a single tile: those scores are never used)
   }
 
   // ---- main loop, software-pipelined over tiles; every MFMA is followed by about six issue slots of
@@ -874,8 +978,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     const unsigned st_k2 = (st_cur + 2 * kStageB >= STAGES * kStageB) ? st_cur + 2 * kStageB - STAGES * kStageB
                                                                        : st_cur + 2 * kStageB;   // stage of tile j+2
     const unsigned st_next = st_cur + kStageB == STAGES * kStageB ? 0 : st_cur + kStageB;
-    const unsigned ring_k2 = ring_cur + 2 * kRingTile >= kRing ? ring_cur + 2 * kRingTile - kRing : ring_cur + 2 * kRingTile;
-    const unsigned lat_cur = MX4 ? ring_cur : st_cur, lat_k2 = MX4 ? ring_k2 : st_k2;
+    const unsigned lat_cur = MX4 ? ring_cur : st_cur;
 
     __builtin_amdgcn_sched_barrier(0);
     if (MX4) {   // this wave's loads of tile j+2 have landed (tiles j+3 .. j+STAGES may be in flight)
@@ -887,6 +990,32 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     // tile 1) and the bf16 rounding of pair i-1; MFMA 16+q carries the LDS transpose reads of V operand q.
     // (Measured: moving the roundings behind the MFMAs of the transpose reads instead costs 25 cycles per tile.)
     float pr[4];
+    if constexpr (MX4) {
+      // MX4: 16 score MFMAs, eight over the codes (64 channels and one term of the queries each) and eight over the RoPE
+      // channels; every one carries a pair of exponentials and the rounding of the pair before, MFMAs 6 .. 13 the transpose reads
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int nt = i & 1, ks = i >> 2, term = (i >> 1) & 1;
+        f32x16& acc = nt == 0 ? n0 : n1;
+        if (i < 2) score_mx_first(acc, qmx[nt][0][0], qmx_sc[nt], negm[nt]);
+        else if (i < 8) score_mx(acc, ks, term, qmx[nt][ks][term], qmx_sc[nt]);
+        else score_mfma(acc, ka[8 + ((i - 8) >> 1)], qreg[nt][8 + ((i - 8) >> 1)]);
+        if (i == 3) { hold(va[1][2]); hold(va[1][3]); hold(pb0[1]); hold(pb1[1]); }
+        if (i == 8) hold_raw(kraw[0]);
+        if (i == 12) { hold_raw(kraw[1]); asm volatile("" : : "v"(ksc)); }
+        if (i == 14) hold(ka[8]);
+        if (i < 8) prob_exp(c0, 2 * i, pr[2 * (i & 1)], pr[2 * (i & 1) + 1]);
+        else prob_exp(c1, 2 * (i - 8), pr[2 * (i & 1)], pr[2 * (i & 1) + 1]);
+        if (i >= 1) {
+          const int pi = i - 1;
+          if (pi < 8) prob_pack(2 * pi, pr[2 * (pi & 1)], pr[2 * (pi & 1) + 1], pb0);
+          else prob_pack(2 * (pi - 8), pr[2 * (pi & 1)], pr[2 * (pi & 1) + 1], pb1);
+        }
+        if (i == 15) prob_pack(14, pr[2], pr[3], pb1);
+        if (i >= 6 && i < 14) load_v_part(lat_cur, (i - 6) >> 2, (i - 6) & 3, va);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
 #pragma unroll
     for (int i = 0; i < 24; ++i) {
       const int ks = i >> 1;
@@ -911,16 +1040,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         const int q = i - 16;
         load_v_part(lat_cur, q >> 2, q & 3, va);
       }
-      if (MX4) {
-        // units of tile j+2: read one MFMA after another, widened and written two MFMAs each once they have arrived
-        if (i < kUnits) widen_read(st_k2, i);
-        const int u = (i - 7) >> 1;
-        if (i >= 7 && u < kUnits) {
-          widen_half(u, (i - 7) & 1);
-          if ((i - 7) & 1) widen_write(lat_k2, u);
-        }
-      }
       __builtin_amdgcn_sched_barrier(0);
+    }
     }
 
     // GLA: this wave's partial scores of tile j+1 go to the exchange buffer (complete only now: the
@@ -986,6 +1107,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         for (int e = 0; e < 4; ++e) { dst[r0 + e] += x0[e]; dst[r0 + 4 + e] += x1[e]; }
         if (m == 5) __builtin_amdgcn_s_barrier();
       }
+      if (MX4 && m == 0) hold(ka[9]);
       if (m == 1) hold(ka[10]);
       if (m == 3) hold(ka[11]);
       if (m >= 5 && m <= 11 && (m & 1) == 1) hold(va[0][(m - 5) >> 1]);   // last read by MFMA m - 4
@@ -993,7 +1115,27 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       if (m == 15) hold(va[1][1]);
       if (m == 10) hold(pb0[0]);
       if (m == 11) hold(pb1[0]);
-      if (m >= 2 && m <= 13) load_k_part(st_k2, lat_k2, m - 2, ka);
+      if (MX4) {
+        // K operands of tile j+2, and its widening into the ring's tile that V(j) has left: units read first, then widened and
+        // written one after the other
+        if (m >= 2 && m <= 8) load_kx_part(st_k2, m - 2, ka);
+        if (m == 12) ksc >>= 8 * g;
+        if (m >= 2 && m <= 5) {
+          widen_read(st_k2, m - 2);
+          if (PAIRED) widen_read(st_k2, m + 2);
+        }
+        if (PAIRED && m >= 7 && m <= 14) {
+          widen_half(m - 7, 0);
+          widen_half(m - 7, 1);
+          widen_write(lat_cur, m - 7);
+        }
+        if (!PAIRED && m >= 7 && m <= 14) {
+          widen_half((m - 7) >> 1, (m - 7) & 1);
+          if ((m - 7) & 1) widen_write(lat_cur, (m - 7) >> 1);
+        }
+      } else if (m >= 2 && m <= 13) {
+        load_k_part(st_k2, st_k2, m - 2, ka);
+      }
       // (the score chains ended four MFMAs and a barrier before MFMA 2; in the GLA form the partner's partial
       // scores are added behind MFMAs 2..5 first)
       constexpr int kMaxAt = GLA ? 6 : 2;
@@ -1020,7 +1162,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       rescale(std::integral_constant<int, 1>{}, need1 ? mx1 : 0.f, n1);
     }
     st_cur = st_next;
-    if (MX4) ring_cur = ring_cur + kRingTile == kRing ? 0 : ring_cur + kRingTile;
+    if (MX4) ring_cur ^= kRingTile;
   };
   {
     const std::integral_constant<bool, true> issuing;
@@ -1179,7 +1321,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 constexpr int kStages = 6;         // plain form: 6 x 24 KiB
 constexpr int kStagesPaired = 4;   // PAIRED form: 4 x 40 KiB = all 160 KiB of LDS
 constexpr int kStagesMx4 = 8;         // MX4, plain: 8 x 13 KiB behind a ring of 48 KiB
-constexpr int kStagesPairedMx4 = 3;   // MX4, PAIRED: 3 x 17 KiB behind a ring of 96 KiB
+constexpr int kStagesPairedMx4 = 5;   // MX4, PAIRED: 5 x 17 KiB behind a ring of 64 KiB
 
 }  // namespace
 
@@ -1282,7 +1424,7 @@ int launch_decode_gla(const DecodeArgs& a) {
 template <int STAGES, int MODE, bool MX4>
 static int launch_form(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) {
   constexpr int blocks = MODE == 1 ? 2 : 1;
-  constexpr int lds = MX4 ? 3 * blocks * kLatBytes + STAGES * (blocks * kTile * kDcb / 2 + 1024 + kRopeBytes)
+  constexpr int lds = MX4 ? mx4_ring_bytes(blocks) + STAGES * (blocks * kTile * kDcb / 2 + 1024 + kRopeBytes)
                           : STAGES * (blocks * kLatBytes + kRopeBytes);
   static_assert(lds <= 160 * 1024, "LDS of a compute unit");
   static PerDeviceSetup setup;
