@@ -245,6 +245,10 @@ __device__ __forceinline__ f32x4 acc_read4() {
 
 // The bf16 ring of the MX4 forms: two tiles, and room for the queries (48 KiB, or 40 KiB) before the first.
 constexpr int mx4_ring_bytes(int blocks) { return blocks == 1 ? 3 * kLatBytes : 4 * kLatBytes; }
+// ... whose 16-byte chunk c of row t lies at chunk position c ^ ring_swz(t): four consecutive rows put a run of four chunks on
+// four different quarters of the banks (transpose reads), and the same chunk of four neighbouring groups of channels of four
+// consecutive rows on sixteen different positions (writes).
+__device__ __forceinline__ int ring_swz(int t) { return (t & 3) * 5; }
 typedef __attribute__((ext_vector_type(6))) unsigned u32x6;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
@@ -262,9 +266,11 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   constexpr int kLatRow = GLA ? 2 * kDcb * 2 : kDcb * 2;    // bytes of one cached latent row of a block
   constexpr int kBlocksWG = PAIRED ? 2 : 1;                 // latent tiles that share a stage
   constexpr int kRowB = MX4 ? kDcb / 2 : kLatRow;           // ... as it is cached
-  constexpr int kRawBytes = kTile * kRowB;                  // (MX4) codes of one block's tile; 1 KiB of scales behind them
-  constexpr int kRopeOff = MX4 ? kBlocksWG * kRawBytes + 1024 : kBlocksWG * kLatBytes;   // RoPE tile behind the latent tile(s)
-  constexpr int kStageB = kRopeOff + kRopeBytes;            // 24 KiB, or 40 KiB (MX4: 13 or 17)
+  constexpr int kRopeOff = kBlocksWG * kLatBytes;           // RoPE tile behind the latent tile(s)
+  // (MX4) A stage is four parts of 16 rows, one per wave: codes (1 KiB a block), scales, RoPE rows.  The loads of a part differ
+  // by instruction offsets, which move both sides, from pointers that are so much lower.
+  constexpr int kXScales = kBlocksWG * 1024, kXRope = kXScales + 256, kXPart = kXRope + kRopeBytes / 4;
+  constexpr int kStageB = MX4 ? 4 * kXPart : kRopeOff + kRopeBytes;   // 24 KiB, or 40 KiB (MX4: 13 or 17)
   constexpr int kLoadsTile = MX4 ? kBlocksWG + 3 : 4 * kBlocksWG + 2;   // direct-to-LDS loads per wave and tile
   constexpr int kRingTile = MX4 ? kBlocksWG * kLatBytes : 0;   // (MX4) one tile of the bf16 ring, in front of the stages
   constexpr int kRing = MX4 ? mx4_ring_bytes(kBlocksWG) : 0;
@@ -423,7 +429,9 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   const unsigned raw_piece = ((lane & 3) ^ ((lane >> 4) & 3)) << 4;
   const unsigned sc_page_bytes = (unsigned)p.n_blocks * (unsigned)p.page_size * (unsigned)kScaleRow;
   const unsigned sc_plane = PAIRED ? ((lane >> 4) & 1) * (unsigned)p.page_size * (unsigned)kScaleRow : 0u;
-  const char* sc_blk = (const char*)p.scales + (size_t)blk0 * p.page_size * kScaleRow;
+  const unsigned raw_voff = (lane >> 2) * kRowB + raw_piece, sc_voff = (lane & 15) * kScaleRow + sc_plane;
+  const char* sc_blk = (const char*)p.scales + (size_t)blk0 * p.page_size * kScaleRow - kXScales;
+  const char* const rope_base = (const char*)p.rope - (MX4 ? kXRope : 0);
   // slot, inside its page, of this wave's first row of the next full tile to issue (they go in order)
   int issue_slot = (t0 + 16 * (int)wave_u) % p.page_size;
   int issue_stage = 0;
@@ -439,20 +447,19 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     // start of this wave's 16 latent rows (block plane blk0) and RoPE rows of the tile inside the page
     iss_lat = lat_blk + (unsigned long long)page * lat_page_bytes + (unsigned)issue_slot * (unsigned)kRowB;
     if (MX4) iss_sc = sc_blk + (unsigned long long)page * sc_page_bytes + (unsigned)issue_slot * (unsigned)kScaleRow;
-    iss_rope = (const char*)p.rope + (unsigned long long)page * rope_page_bytes + (unsigned)issue_slot * (unsigned)(kDr * 2);
+    iss_rope = rope_base + (unsigned long long)page * rope_page_bytes + (unsigned)issue_slot * (unsigned)(kDr * 2);
     iss_stage = stage_base + stage_off;
   };
   // parts 0..3 = latent loads (PAIRED: 4..7 = the second block's; MX4: codes of each block, then scales), then two RoPE loads
   auto issue_full_part = [&](int part) {
-    if (MX4 && part <= kBlocksWG) {
-      if (part < kBlocksWG) {
-        set_m0(iss_stage + part * kRawBytes + wave_u * 1024);
-        lds_dma16<0>(iss_lat + part * lat_plane_bytes, (lane >> 2) * kRowB + raw_piece);
-      } else {
-        set_m0(iss_stage + kBlocksWG * kRawBytes + wave_u * 256);
-        lds_dma4(iss_sc, (lane & 15) * kScaleRow + sc_plane);
-      }
-    } else if (!MX4 && part < 4 * kBlocksWG) {
+    if (MX4) {
+      if (part == 0) set_m0(iss_stage + wave_u * kXPart);
+      if (part == 0) lds_dma16<0>(iss_lat, raw_voff);
+      else if (part < kBlocksWG) lds_dma16<1024>(iss_lat + (lat_plane_bytes - 1024), raw_voff);
+      else if (part == kBlocksWG) lds_dma4<kXScales>(iss_sc, sc_voff);
+      else if (part == kBlocksWG + 1) lds_dma16<kXRope>(iss_rope, rope_voff[0]);
+      else lds_dma16<kXRope + 1024>(iss_rope, rope_voff[1]);
+    } else if (part < 4 * kBlocksWG) {
       const int jb = part >> 2, q = part & 3;
       const char* src = iss_lat + jb * lat_half_step;
       if (q == 0) set_m0(iss_stage + jb * kLatBytes + wave_u * 4096);
@@ -499,13 +506,14 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     const char* src_rope = (const char*)p.rope + (unsigned long long)page * rope_page_bytes + (unsigned)slot * (unsigned)(kDr * 2);
     const unsigned stage = stage_base + issue_stage * kStageB;
     if (MX4) {
+      const unsigned part = stage + wave_u * kXPart;
 #pragma unroll
       for (int jb = 0; jb < kBlocksWG; ++jb) {
-        set_m0(stage + jb * kRawBytes + wave_u * 1024);
+        set_m0(part + jb * 1024);
         lds_dma16<0>(src_lat + jb * lat_half_step, (unsigned)(min(w0 + (lane >> 2), last) - first) * kRowB + raw_piece);
       }
-      set_m0(stage + kBlocksWG * kRawBytes + wave_u * 256);
-      lds_dma4(sc_blk + (unsigned long long)page * sc_page_bytes + (unsigned)slot * (unsigned)kScaleRow,
+      set_m0(part);
+      lds_dma4<kXScales>(sc_blk + (unsigned long long)page * sc_page_bytes + (unsigned)slot * (unsigned)kScaleRow,
                (unsigned)(min(w0 + (lane & 15), last) - first) * kScaleRow + sc_plane);
     }
 #pragma unroll
@@ -521,7 +529,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     for (int q = 0; q < 2; ++q) {
       const int t = (wave * 2 + q) * 8 + (lane >> 3);          // 0..63
       const unsigned row = (unsigned)(min(t, last) - first);
-      set_m0(stage + kRopeOff + wave_u * 2048 + q * 1024);
+      set_m0(MX4 ? stage + wave_u * kXPart + kXRope + q * 1024 : stage + kRopeOff + wave_u * 2048 + q * 1024);
       lds_dma16<0>(src_rope, row * (kDr * 2) + (((lane & 7) ^ rope_swz(t)) << 4));
     }
     issue_stage = (issue_stage + 1 == STAGES) ? 0 : issue_stage + 1;
@@ -534,14 +542,16 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   const int s_tok = tw * 32 + c32;
   const unsigned own_lat = PAIRED ? hw * kLatBytes : 0;   // this wave's block inside a stage
   const unsigned k_lat_off = own_lat + s_tok * (kDcb * 2) + ((g ^ lat_swz(s_tok)) << 4);      // ^ (ks << 5)
-  const unsigned k_rope_off = kRopeOff + s_tok * (kDr * 2) + ((g ^ rope_swz(s_tok)) << 4);    // ^ (ks << 5)
+  const unsigned k_rope_off = (MX4 ? (s_tok >> 4) * kXPart + kXRope + (s_tok & 15) * (kDr * 2) : kRopeOff + s_tok * (kDr * 2)) +
+                              ((g ^ rope_swz(s_tok)) << 4);                                   // ^ (ks << 5)
   unsigned v_off[2];                                                          // ^ (mt << 6), + 4096 ss
   {
     const int k = (lane & 15) >> 2, seg = lane & 3, hb = (lane >> 4) & 1;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int ta = tw * 32 + 8 * half + 4 * g + k;
-      v_off[half] = own_lat + ta * (kDcb * 2) + (((2 * hb + (seg >> 1)) ^ lat_swz(ta)) << 4) + ((seg & 1) << 3);
+      v_off[half] = own_lat + ta * (kDcb * 2) + (((2 * hb + (seg >> 1)) ^ (MX4 ? ring_swz(ta) : lat_swz(ta))) << 4) +
+                    ((seg & 1) << 3);
     }
   }
 
@@ -581,8 +591,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // instruction applies itself; byte 2 ks of ksc is the scale of operand ks
   mx4_tile::u32x4 kraw[2];
   unsigned ksc = 0;
-  const unsigned kx_off = (PAIRED ? hw * kRawBytes : 0) + s_tok * kRowB + ((g ^ ((s_tok >> 2) & 3)) << 4);
-  const unsigned kx_sc = kBlocksWG * kRawBytes + (s_tok >> 4) * 256 + (PAIRED ? hw * 64 : 0) + (s_tok & 15) * kScaleRow;
+  const unsigned kx_off = (s_tok >> 4) * kXPart + (PAIRED ? hw * 1024 : 0) + (s_tok & 15) * kRowB + ((g ^ ((s_tok >> 2) & 3)) << 4);
+  const unsigned kx_sc = (s_tok >> 4) * kXPart + kXScales + (PAIRED ? hw * 64 : 0) + (s_tok & 15) * kScaleRow;
   auto load_kx_part = [&](unsigned st_off, int part, bf16x8 (&ka)[12]) {   // 0, 1: codes; 2: scales; 3 .. 6: RoPE
     typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
     typedef const __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
@@ -605,45 +615,44 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     const short4v hi = lds_tr16(hi_p + ss * 16 * (kDcb * 2));
     va[ss][mt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  // (MX4) Widening of the wave's own 16 rows of a tile: unit u = 4 jb + i is the rows 4 i .. 4 i + 3 of block jb, a lane has
-  // eight channels (row lane / 16, 16-byte chunk lane % 16 of the bf16 row).  Reads are linear; the chunks of a row that
-  // sixteen lanes write lie in sixteen different bank groups.
-  constexpr int kUnits = MX4 ? 4 * kBlocksWG : 0;
-  const unsigned cv_codes = wave * 1024 + lane * 4;
-  const unsigned cv_scale = kBlocksWG * kRawBytes + wave * 256 + (lane >> 4) * kScaleRow + ((lane >> 2) & 3);
-  const unsigned cv_out = (16 * wave + (lane >> 4)) * (kDcb * 2) + (((lane & 15) ^ ((lane >> 4) << 2)) << 4);
-  unsigned cv_raw[8], cv_byte[8];
-  mx4_tile::u32x4 cv_val;
-  auto widen_read = [&](unsigned st_off, int u) {
-    typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
-    const int jb = u >> 2, i = u & 3;
-    cv_raw[u] = *(u32_ptr)(size_t)(((stage_base + st_off + cv_codes) ^ (i << 4)) + jb * kRawBytes + i * 256);
-    cv_byte[u] = *(lds_byte_ptr)(size_t)(stage_base + st_off + cv_scale + jb * 64 + i * 16);
+  // (MX4) Widening of the wave's own 16 rows of a tile, a block at a time: a lane has one group, 16 bytes of codes and their
+  // scale (row lane / 4, group lane % 4), and writes four 16-byte chunks of the bf16 row.  Reads are linear; the ring's swizzle
+  // puts the chunks that sixteen lanes (four rows) write into sixteen different bank groups.
+  const unsigned cv_codes = wave * kXPart + (lane >> 2) * kRowB + raw_piece;
+  const unsigned cv_scale = wave * kXPart + kXScales + lane;
+  const unsigned cv_out = (16 * wave + (lane >> 2)) * (kDcb * 2) + (((lane & 3) << 2 ^ ring_swz(lane >> 2)) << 4);
+  mx4_tile::u32x4 cv_raw[2], cv_val;
+  unsigned cv_byte[2];
+  auto widen_read = [&](unsigned st_off, int jb) {
+    typedef const __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
+    cv_raw[jb] = *(u32x4_ptr)(size_t)(stage_base + st_off + cv_codes + jb * 1024);
+    cv_byte[jb] = *(lds_byte_ptr)(size_t)(stage_base + st_off + cv_scale + jb * 64);
   };
-  auto widen_half = [&](int u, int half) {       // four of the eight channels
-    const float scale = mx4_tile::scale_of(cv_byte[u]);
+  auto widen_half = [&](int jb, int i, int half) {       // four of the eight channels of chunk i
+    const float scale = mx4_tile::scale_of(cv_byte[jb]);
     if (half == 0) {
-      cv_val[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 0));
-      cv_val[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 1));
+      cv_val[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[jb][i], scale, 0));
+      cv_val[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[jb][i], scale, 1));
     } else {
-      cv_val[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 2));
-      cv_val[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[u], scale, 3));
+      cv_val[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[jb][i], scale, 2));
+      cv_val[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cv_raw[jb][i], scale, 3));
     }
   };
-  auto widen_write = [&](unsigned lat_off, int u) {
+  auto widen_write = [&](unsigned lat_off, int jb, int i) {
     typedef __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
-    const int jb = u >> 2, i = u & 3;
-    *(u32x4_ptr)(size_t)(((lds_base + lat_off + cv_out) ^ (i << 4)) + jb * kLatBytes + i * 1024) = cv_val;
+    *(u32x4_ptr)(size_t)(((lds_base + lat_off + cv_out) ^ (i << 4)) + jb * kLatBytes) = cv_val;
   };
   auto widen_tile = [&](unsigned st_off, unsigned lat_off) {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) widen_read(st_off, u);
+    for (int jb = 0; jb < kBlocksWG; ++jb) widen_read(st_off, jb);
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      widen_half(u, 0);
-      widen_half(u, 1);
-      widen_write(lat_off, u);
-    }
+    for (int jb = 0; jb < kBlocksWG; ++jb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        widen_half(jb, i, 0);
+        widen_half(jb, i, 1);
+        widen_write(lat_off, jb, i);
+      }
   };
   // Column maxima.  In the accumulator layout a lane holds 16 of the 32 token rows of its head column
   // and the lane 32 away holds the other 16.  max8 folds eight more rows into a running maximum;
@@ -1120,18 +1129,16 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         // written one after the other
         if (m >= 2 && m <= 8) load_kx_part(st_k2, m - 2, ka);
         if (m == 12) ksc >>= 8 * g;
-        if (m >= 2 && m <= 5) {
-          widen_read(st_k2, m - 2);
-          if (PAIRED) widen_read(st_k2, m + 2);
-        }
+        if (m == 2) widen_read(st_k2, 0);
+        if (PAIRED && m == 4) widen_read(st_k2, 1);
         if (PAIRED && m >= 7 && m <= 14) {
-          widen_half(m - 7, 0);
-          widen_half(m - 7, 1);
-          widen_write(lat_cur, m - 7);
+          widen_half((m - 7) >> 2, (m - 7) & 3, 0);
+          widen_half((m - 7) >> 2, (m - 7) & 3, 1);
+          widen_write(lat_cur, (m - 7) >> 2, (m - 7) & 3);
         }
         if (!PAIRED && m >= 7 && m <= 14) {
-          widen_half((m - 7) >> 1, (m - 7) & 1);
-          if ((m - 7) & 1) widen_write(lat_cur, (m - 7) >> 1);
+          widen_half(0, (m - 7) >> 1, (m - 7) & 1);
+          if ((m - 7) & 1) widen_write(lat_cur, 0, (m - 7) >> 1);
         }
       } else if (m >= 2 && m <= 13) {
         load_k_part(st_k2, st_k2, m - 2, ka);
@@ -1424,7 +1431,7 @@ int launch_decode_gla(const DecodeArgs& a) {
 template <int STAGES, int MODE, bool MX4>
 static int launch_form(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) {
   constexpr int blocks = MODE == 1 ? 2 : 1;
-  constexpr int lds = MX4 ? mx4_ring_bytes(blocks) + STAGES * (blocks * kTile * kDcb / 2 + 1024 + kRopeBytes)
+  constexpr int lds = MX4 ? mx4_ring_bytes(blocks) + STAGES * (4 * (blocks * 1024 + 256) + kRopeBytes)
                           : STAGES * (blocks * kLatBytes + kRopeBytes);
   static_assert(lds <= 160 * 1024, "LDS of a compute unit");
   static PerDeviceSetup setup;

@@ -86,9 +86,10 @@ __device__ __forceinline__ void lds_dma16(const void* sbase, unsigned voff) {
   asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" : : "v"(voff), "s"(sbase), "n"(OFF) : "memory");
 }
 
-// four bytes a lane, to m0 + 4 i
+// four bytes a lane, to m0 + OFF + 4 i
+template <int OFF>
 __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff) {
-  asm volatile("global_load_lds_dword %0, %1" : : "v"(voff), "s"(sbase) : "memory");
+  asm volatile("global_load_lds_dword %0, %1 offset:%2" : : "v"(voff), "s"(sbase), "n"(OFF) : "memory");
 }
 
 __device__ __forceinline__ short4v lds_tr16(const __attribute__((address_space(3))) unsigned char* p) {

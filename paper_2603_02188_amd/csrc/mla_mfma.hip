@@ -496,7 +496,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
       lds_dma16<0>(iss_lat, min(8 * wave + 4 * i + (lane >> 4), last) * kXRow + (lane & 15) * 16);
     } else if (i == 2) {
       set_m0(iss_dst + kXScales + wave_u * 256);
-      lds_dma4(iss_sc, min(8 * wave + ((lane >> 2) & 7), last) * kXScaleRow + (lane & 3) * 4);
+      lds_dma4<0>(iss_sc, min(8 * wave + ((lane >> 2) & 7), last) * kXScaleRow + (lane & 3) * 4);
     } else {
       const int t = 8 * wave + (lane >> 3);
       set_m0(iss_dst + kRopeOff + wave_u * 1024);
