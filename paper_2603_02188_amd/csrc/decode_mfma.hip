@@ -249,10 +249,7 @@ constexpr int mx4_ring_bytes(int blocks) { return blocks == 1 ? 3 * kLatBytes : 
 // four different quarters of the banks (transpose reads), and the same chunk of four neighbouring groups of channels of four
 // consecutive rows on sixteen different positions (writes).
 __device__ __forceinline__ int ring_swz(int t) { return (t & 3) * 5; }
-typedef __attribute__((ext_vector_type(6))) unsigned u32x6;
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
-typedef __attribute__((ext_vector_type(32))) float f32x32;
+using mx4_tile::u32x6;
 
 // What a workgroup costs beside its tiles (start-up, write-out), in tiles of about 1.1 us: sections of its life in the
 // 16-tile launch of 16 sequences of 16K tokens.
@@ -827,35 +824,18 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       qaddr[8 + ks] = (!GLA || (ks >> 1) == hw) ? addr : lds_base + STAGES * kStageB;
     }
     if (MX4) {
-      // A lane's 32 channels of operand ks are one group of the other side, channels 64 ks + 32 g .. + 31: a query there is
-      // hi + lo, E2M3 numbers (four significant bits, up to 7.5) with a power of two each, 2^-5 apart.  What is left is
-      // 2^-10 of the group's largest channel at most, less than a query in bf16 is off in the mean (0.11 % against 0.165 %).
+      // a lane's 32 channels of operand ks, 64 ks + 32 g .. + 31, are one group
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        bf16x32 x;
-        unsigned top = 0;
-        f32x32 v;
+        mx4_tile::f32x32 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const bf16x8 part = *(lds_bf16x8_ptr)(size_t)(q_lds + row * (kDcb * 2) + (((8 * ks + 4 * g + i) ^ (row & 15)) << 4));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v[8 * i + e] = (float)part[e] * sc;
-            top = max(top, __float_as_uint(v[8 * i + e]) & 0x7fffffffu);
-          }
+          for (int e = 0; e < 8; ++e) v[8 * i + e] = (float)part[e] * sc;
         }
-        // (7.5 is the largest: from 1.875 2^e on the next power of two; a group with an infinity or a NaN is NaN)
-        const int ex = min(max((int)((top + 0x100000u) >> 23) - 2, 7), 252);
-        const bool finite = top < 0x7f800000u;
-        const float s_hi = __uint_as_float((unsigned)ex << 23), s_lo = __uint_as_float((unsigned)(ex - 5) << 23);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = (__bf16)v[e];
-        u32x6 hi = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, s_hi);
-        const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(hi, s_hi);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = (__bf16)(v[e] - back[e]);
-        u32x6 lo = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, s_lo);
-        qmx_sc[nt] |= (finite ? (unsigned)ex | (unsigned)(ex - 5) << 8 : 0xffffu) << (16 * ks);
+        u32x6 hi, lo;
+        qmx_sc[nt] |= mx4_tile::split_query(v, hi, lo) << (16 * ks);
         asm volatile("" : "+a"(hi), "+a"(lo));
         qmx[nt][ks][0] = hi;
         qmx[nt][ks][1] = lo;
@@ -899,16 +879,14 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     if (MX4) {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        const i32x8 kt = {(int)kraw[ks][0], (int)kraw[ks][1], (int)kraw[ks][2], (int)kraw[ks][3], 0, 0, 0, 0};
+        const mx4_tile::i32x8 kt = mx4_tile::operand(kraw[ks]);
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
           for (int term = 0; term < 2; ++term) {
-            const u32x6 q = qmx[nt][ks][term];
-            const i32x8 qt = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0};
             f32x16& acc = nt == 0 ? sa0 : sa1;
-            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kt, qt, acc, 4, 2, 0, ksc >> (16 * ks), 0,
-                                                                  qmx_sc[nt] >> (16 * ks + 8 * term));
+            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kt, mx4_tile::operand(qmx[nt][ks][term]), acc, 4, 2, 0,
+                                                                  ksc >> (16 * ks), 0, qmx_sc[nt] >> (16 * ks + 8 * term));
           }
       }
     }

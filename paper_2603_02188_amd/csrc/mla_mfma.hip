@@ -427,12 +427,13 @@ constexpr int kPStages = 4;
 constexpr int kPPOff = kPStages * kMStage, kPAOff = kPPOff + 2 * kMPBytes, kPXOff = kPAOff + 2 * kMHeads * 4,
               kPFOff = kPXOff + 2 * 4 * 32 * 4, kPLds = kPFOff + 2 * 4 * 4;
 static_assert(kPLds <= 160 * 1024, "one workgroup per CU");
-// Latent cache in 4 bits: the stages hold codes, scales (1 KiB) and RoPE rows as they lie in memory, 13 KiB; behind what is
-// above, a ring of three tiles holds the latent channels widened to bf16.  A wave widens the eight rows that it loaded
-// itself, tile j + 2 during the scores of step j; the barrier behind them hands the rows to the others.
+// Latent cache in 4 bits: the stages hold codes, scales (1 KiB) and RoPE rows as they lie in memory, 13 KiB.  The scores take the
+// codes as they are (v_mfma_scale_f32_16x16x128_f8f6f4, the queries as sums of two E2M3 numbers: see decode_mfma.hip); for the
+// value product two tiles, behind what is above, hold the latent channels widened to bf16.  A wave widens the eight rows that it
+// loaded itself: read behind the value product of step j, tile j + 2 is converted and written during the scores of step j + 1.
 constexpr int kXRow = kMDc / 2, kXScaleRow = kMDc / mx4_tile::kGroup, kXScales = kMTok * kXRow, kXRope = kXScales + 1024,
               kXStage = kXRope + kMRopeBytes, kXLoads = 4;
-constexpr int kXRing = kPStages * kXStage, kXShift = kXRing + 3 * kMLatBytes - kPPOff;   // (the tables move up by kXShift)
+constexpr int kXRing = kPStages * kXStage, kXShift = kXRing + 2 * kMLatBytes - kPPOff;   // (the tables move up by kXShift)
 constexpr int kXLds = kPLds + kXShift;
 static_assert(kXLds <= 160 * 1024, "one workgroup per CU");
 
@@ -493,7 +494,9 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   auto issue_part_mx4 = [&](int i, int last) {
     if (i < 2) {
       set_m0(iss_dst + wave_u * (8 * kXRow) + i * 1024);
-      lds_dma16<0>(iss_lat, min(8 * wave + 4 * i + (lane >> 4), last) * kXRow + (lane & 15) * 16);
+      // (piece p of row t lies at position p ^ t % 16: sixteen rows' reads of one piece hit sixteen different bank groups)
+      const int t = 8 * wave + 4 * i + (lane >> 4);
+      lds_dma16<0>(iss_lat, min(t, last) * kXRow + (((lane ^ t) & 15) << 4));
     } else if (i == 2) {
       set_m0(iss_dst + kXScales + wave_u * 256);
       lds_dma4<0>(iss_sc, min(8 * wave + ((lane >> 2) & 7), last) * kXScaleRow + (lane & 3) * 4);
@@ -540,13 +543,29 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
 
   // ---- query operands of this wave's 32 heads, two groups of 16
   bf16x8 qreg[2][18];
+  mx4_tile::u32x6 qmx[2][4][2];    // (4 bits) [group][128 channels][term], a lane's 32 channels are one group of the cache's side
+  unsigned qmx_sc[2][4] = {};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int head = min(head_base + 32 * hg + 16 * i + c16, p.h - 1);
     const bf16_t* qa = p.q_abs + ((size_t)seq * p.h + head) * kMDc + q4 * 8;
     const bf16_t* qr = p.q_rope + ((size_t)seq * p.h + head) * kDr + q4 * 8;
+    if constexpr (MX4) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        mx4_tile::f32x32 v;
+#pragma unroll
+        for (int e8 = 0; e8 < 4; ++e8) {
+          const bf16x8 part = *(const bf16x8*)(qa + ks * 128 + q4 * 24 + e8 * 8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[8 * e8 + e] = (float)part[e];
+        }
+        qmx_sc[i][ks] = mx4_tile::split_query(v, qmx[i][ks][0], qmx[i][ks][1]);
+      }
+    } else {
 #pragma unroll
     for (int ks = 0; ks < 16; ++ks) qreg[i][ks] = *(const bf16x8*)(qa + ks * 32);
+    }
     qreg[i][16] = *(const bf16x8*)qr;
     qreg[i][17] = *(const bf16x8*)(qr + 32);
   }
@@ -560,9 +579,12 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   issue_whole();
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 2; ++i) {
 #pragma unroll
-    for (int ks = 0; ks < 18; ++ks) asm volatile("" : "+a"(qreg[i][ks]));
+    for (int ks = MX4 ? 16 : 0; ks < 18; ++ks) asm volatile("" : "+a"(qreg[i][ks]));
+#pragma unroll
+    for (int ks = 0; ks < (MX4 ? 4 : 0); ++ks) asm volatile("" : "+a"(qmx[i][ks][0]), "+a"(qmx[i][ks][1]));
+  }
   __builtin_amdgcn_sched_barrier(0);
   const int n_pro = min(ntiles, kPStages);
   for (int jj = 1; jj < n_pro; ++jj) issue_whole();
@@ -576,7 +598,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   unsigned v_off;                                                             // ^ (mt << 6), + 16 KiB ss
   {
     const int k = (lane & 15) >> 2, seg = lane & 3, hb = (lane >> 4) & 1, ta = 4 * g + k;
-    v_off = ta * 1024 + wave * 256 + (((2 * hb + (seg >> 1)) ^ lat_swz(ta)) << 4) + ((seg & 1) << 3);
+    v_off = ta * 1024 + wave * 256 + (((2 * hb + (seg >> 1)) ^ lat_swz(ta) ^ (MX4 ? wave : 0)) << 4) + ((seg & 1) << 3);
   }
   // this lane's four probabilities of head group i go to + 256 i
   const unsigned p_wr_off = hg * 2048 + th * 1024 + (c16 + 32 * (q4t & 1)) * 16 + (q4t >> 1) * 8;
@@ -614,50 +636,84 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   auto p_read = [&](int par, int i) {           // i = 2 nt + ss
     pb[i & 1][i >> 1] = *(const bf16x8*)(smem + kPP + par * kMPBytes + i * 1024 + lane * 16);
   };
-  // (4 bits) unit u of a tile: row 8 wave + u, eight channels a lane
-  const unsigned wd_out[2] = {(unsigned)(lane * 16 ^ ((2 * wave) & 3) << 4), (unsigned)(lane * 16 ^ ((2 * wave + 1) & 3) << 4)};
-  unsigned wd_raw[8], wd_byte[8];
-  auto widen_read = [&](unsigned base, int u) {
-    typedef const __attribute__((address_space(3))) unsigned* u32_ptr;
-    wd_raw[u] = *(u32_ptr)(size_t)(base + wave * (8 * kXRow) + u * kXRow + lane * 4);
-    wd_byte[u] = *(lds_byte_ptr)(size_t)(base + kXScales + wave * 256 + u * kXScaleRow + (lane >> 2));
+  // (4 bits) K operands of a tile: codes of 128 channels (parts 0 .. 3), scales (4), RoPE (5, 6)
+  const unsigned kx_off = (16 * th + k_tok) * kXRow + ((q4 ^ k_tok) << 4);                                // ^ (ks << 6)
+  const unsigned kx_sc_off = kXScales + ((16 * th + k_tok) >> 3) * 256 + (k_tok & 7) * kXScaleRow;
+  mx4_tile::u32x4 kx[4], kx_sc;
+  auto kx_read = [&](unsigned base, int part) {
+    typedef const __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
+    if (part < 4) kx[part] = *(u32x4_ptr)(size_t)((base + kx_off) ^ (part << 6));
+    else if (part == 4) kx_sc = *(u32x4_ptr)(size_t)(base + kx_sc_off);
+    else k_read(base, base, 11 + part);
   };
-  auto widen_write = [&](unsigned lat, int u) {
+  // (4 bits) rows 8 wave + 4 r + lane / 16 of a tile, r = 0, 1: a lane widens one group, four 16-byte chunks.  Group g of row t
+  // lies in quarter g / 4 of the row, chunk c = 4 (g % 4) + i at position c ^ lat_swz(t) ^ g / 4, so that the sixteen groups of a
+  // row are written to sixteen different bank groups.
+  unsigned wd_out[2], wd_sc[2], wd_byte[2];
+  mx4_tile::u32x4 wd_raw[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int t = 8 * wave + 4 * r + (lane >> 4), grp = (lane ^ t) & 15;
+    wd_sc[r] = kXScales + wave * 256 + (4 * r + (lane >> 4)) * kXScaleRow + grp;
+    wd_out[r] = t * 1024 + (grp >> 2) * 256 + ((((grp & 3) << 2) ^ lat_swz(t) ^ (grp >> 2)) << 4);       // ^ (i << 4)
+  }
+  auto widen_read = [&](unsigned base, int r) {
+    typedef const __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
+    wd_raw[r] = *(u32x4_ptr)(size_t)(base + (8 * wave + 4 * r) * kXRow + lane * 16);
+    wd_byte[r] = *(lds_byte_ptr)(size_t)(base + wd_sc[r]);
+  };
+  auto widen_write = [&](unsigned lat, int r, int i) {
     typedef __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
-    *(u32x4_ptr)(size_t)(lat + (8 * wave + u) * 1024 + (wd_out[u >> 2] ^ ((u & 3) << 6))) =
-        mx4_tile::decode8(wd_raw[u], mx4_tile::scale_of(wd_byte[u]));
+    *(u32x4_ptr)(size_t)((lat + wd_out[r]) ^ (i << 4)) = mx4_tile::decode8(wd_raw[r][i], mx4_tile::scale_of(wd_byte[r]));
   };
-  auto widen_tile = [&](unsigned base, unsigned lat) {
-    asm volatile("" ::: "memory");
+  // scores of a tile whose operands are read, with the operands of the value product of the tile before it and (with_v) the tile
+  // itself widened into wl
+  auto scores_mx4 = [&](unsigned vb, int par, auto with_v, unsigned wl) {
+    constexpr bool V = decltype(with_v)::value;
+    s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < 8; ++u) widen_read(base, u);
+    for (int i = 0; i < 4; ++i) kx_sc[i] >>= 8 * q4;       // group 4 ks + q4 in byte 0
 #pragma unroll
-    for (int u = 0; u < 8; ++u) widen_write(lat, u);
+    for (int m = 0; m < 10; ++m) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int ks = m >> 1, term = m & 1;
+        if (m < 8)
+          s[i] = term == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_tile::operand(kx[ks & 3]), mx4_tile::operand(qmx[i][ks & 3][0]),
+                                                                             s[i], 4, 2, 0, kx_sc[ks & 3], 0, qmx_sc[i][ks & 3])
+                           : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_tile::operand(kx[ks & 3]), mx4_tile::operand(qmx[i][ks & 3][1]),
+                                                                             s[i], 4, 2, 0, kx_sc[ks & 3], 1, qmx_sc[i][ks & 3]);
+        else
+          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[8 + m], qreg[i][8 + m], s[i], 0, 0, 0);
+      }
+      if (V && m < 8) {
+        v_read(vb, 2 * m);
+        v_read(vb, 2 * m + 1);
+        widen_write(wl, m >> 2, m & 3);
+      }
+      if (V && m >= 5 && m < 9) p_read(par, m - 5);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // scores of a tile (its first operands already read), with the operands of the value product of the tile before it and, ISSUE, the
-  // second half of the loads of the tile after next (4 bits: the tile in wd is widened into wl instead)
-  auto scores = [&](unsigned kb, unsigned kl, unsigned vb, int par, auto with_v, auto issue, bool rest, unsigned wd = 0u,
-                    unsigned wl = 0u) {
+  // second half of the loads of the tile after next
+  auto scores = [&](unsigned kb, unsigned vb, int par, auto with_v, auto issue, bool rest) {
     constexpr bool ISSUE = decltype(issue)::value;
     s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 18; ++m) {
       s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[m], qreg[0][m], s[0], 0, 0, 0);
       s[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[m], qreg[1][m], s[1], 0, 0, 0);
-      if (m + kAhead < 18) k_read(kb, kl, m + kAhead);
+      if (m + kAhead < 18) k_read(kb, kb, m + kAhead);
       if (decltype(with_v)::value && m < 16) v_read(vb, m);
       if (decltype(with_v)::value && m >= 10 && m < 14) p_read(par, m - 10);
-      if (MX4 && decltype(with_v)::value) {
-        if (m < 8) widen_read(wd, m);
-        if (m >= 6 && m < 14) widen_write(wl, m - 6);
-      }
-      if (!MX4 && m % 3 == 1 && m < 15) {
+      if (m % 3 == 1 && m < 15) {
         if (ISSUE) issue_part(4 + m / 3);
         else if (rest) issue_part_any(4 + m / 3);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (!MX4 && (ISSUE || rest)) issue_end();
+    if (ISSUE || rest) issue_end();
   };
   // the tile's maxima over this wave's 16 tokens, for the wave with the other 16 as well
   auto publish_max = [&](int par) {
@@ -732,7 +788,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   auto grown_at = [&](int par) { return *(const int2*)(smem + kPF + par * 16); };   // waves 0, 1: heads 0..31, 32..63
   auto after = [&](unsigned st) { return st == lds_base + (kPStages - 1) * kStageB ? lds_base : st + kStageB; };
   const unsigned ring = lds_base + kXRing;
-  auto ring_after = [&](unsigned at) { return at == ring + 2 * kMLatBytes ? ring : at + kMLatBytes; };
+  auto ring_after = [&](unsigned at) { return at == ring ? ring + kMLatBytes : ring; };
 
   // ---- prologue: scores and probabilities of tile 0
   if (ntiles > 3) wait_vm_lgkm<3 * kLoads>();
@@ -740,22 +796,29 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   else if (ntiles > 1) wait_vm_lgkm<kLoads>();
   else wait_vm_lgkm<0>();
   if (MX4) {
-    widen_tile(lds_base, ring);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      widen_read(lds_base, r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) widen_write(ring, r, i);
+    }
     wait_vm_lgkm<63>();
   }
   hand_over();
-  const unsigned lat0 = MX4 ? ring : lds_base, lat1 = MX4 ? ring + kMLatBytes : lds_base + kStageB;
+  if (MX4) {
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) k_read(lds_base, lat0, i);
-  scores(lds_base, lat0, 0u, 0, std::false_type{}, std::false_type{}, false);
+    for (int i = 0; i < 7; ++i) kx_read(lds_base, i);
+    scores_mx4(0u, 0, std::false_type{}, 0u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) k_read(lds_base, lds_base, i);
+    scores(lds_base, 0u, 0, std::false_type{}, std::false_type{}, false);
+  }
   publish_max(0);
   if (ntiles > 3) wait_vm_lgkm<2 * kLoads>();
   else if (ntiles > 2) wait_vm_lgkm<kLoads>();
   else wait_vm_lgkm<0>();
-  if (MX4) {
-    widen_tile(lds_base + kStageB, lat1);   // (one tile: whatever the stage holds, unused)
-    wait_vm_lgkm<63>();
-  }
   hand_over();                       // the maxima are visible, tile 1 has landed
   if (MX4 && ntiles > kPStages) issue_whole();   // tile 4: the stage of tile 0 is free
   refresh(partner_max(0), 0, 0);
@@ -763,8 +826,16 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   for (int e = 0; e < 4; ++e) soften(e, ntiles == 1 ? nvalid_last : kMTok);
   store_p(0);
   __builtin_amdgcn_sched_barrier(0);
+  // (one tile: whatever the stage holds, unused)
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) k_read(lds_base + kStageB, lat1, i);   // (one tile: whatever the stage holds, unused)
+  for (int i = 0; i < (MX4 ? 7 : kAhead); ++i) {
+    if (MX4) kx_read(lds_base + kStageB, i);
+    else k_read(lds_base + kStageB, lds_base + kStageB, i);
+  }
+  if (MX4) {
+    widen_read(lds_base + kStageB, 0);
+    widen_read(lds_base + kStageB, 1);
+  }
 
   // ---- step j: scores of tile j + 1 while the operands of tile j's value product are read; one barrier; the value product
   // of tile j, with the softmax of tile j + 1 and the first operands of tile j + 2 between its MFMAs; one barrier, behind
@@ -779,8 +850,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     constexpr bool ISSUE = decltype(issue)::value;         // tiles j + 3 and j + 4 (4 bits: j + 5) exist and are no last ones
     const int par = j & 1, next = par ^ 1;
     const unsigned st_next = after(st_cur), st_then = after(st_next);
-    const unsigned ring_next = ring_after(ring_cur), ring_then = ring_after(ring_next);
-    const unsigned lat_cur = MX4 ? ring_cur : st_cur, lat_next = MX4 ? ring_next : st_next, lat_then = MX4 ? ring_then : st_then;
+    const unsigned ring_next = ring_after(ring_cur);
     __builtin_amdgcn_sched_barrier(0);
     if (MX4) {                       // tile j + 2 has landed in this wave's share; j + 3 and j + 4 may be in flight
       if (ISSUE || j + 4 < ntiles) wait_vmcnt<2 * kLoads>();
@@ -788,7 +858,8 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
       asm volatile("" ::: "memory");
     }
     const int2 grown = grown_at(par);
-    scores(st_next, lat_next, lat_cur, par, std::true_type{}, issue, rest, st_then, lat_then);
+    if constexpr (MX4) scores_mx4(ring_cur, par, std::true_type{}, ring_next);
+    else scores(st_next, st_cur, par, std::true_type{}, issue, rest);
     publish_max(next);
     // tile j + 2 has landed in this wave's share, its reads of tile j are done, the maxima are stored
     if (MX4) wait_vm_lgkm<63>();
@@ -811,9 +882,13 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
         if (ISSUE) issue_part(m >> 1);
         else if (rest) issue_part_any(m >> 1);
       }
-      if (m >= 3) {
-        k_read(st_then, lat_then, 2 * (m - 3));
-        k_read(st_then, lat_then, 2 * (m - 3) + 1);
+      if (MX4) {
+        if (m >= 3 && m < 7) kx_read(st_then, 2 * (m - 3));
+        if (m >= 3 && m < 6) kx_read(st_then, 2 * (m - 3) + 1);
+        if (m >= 6) widen_read(st_then, m - 6);
+      } else if (m >= 3) {
+        k_read(st_then, st_then, 2 * (m - 3));
+        k_read(st_then, st_then, 2 * (m - 3) + 1);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
