@@ -285,6 +285,14 @@ MLRA_API int mlra_mx4_append_kv(const mlra_mx4_cache* cache, int32_t batch, int3
 MLRA_API int mlra_mx4_read_kv(const mlra_mx4_cache* cache, int32_t batch, int32_t n_rows, const int32_t* positions,
                      const int32_t* row_lens, void* c_kv_out, void* k_rope_out, int32_t dst_dtype, void* stream);
 
+/* mlra_pre_attention for a cache in 4 bits: the same projections, norms and rotation, whose new rows stay fp32 until
+ * mlra_mx4_append_kv's rounding (positions, weights and outputs as there; slots that do not exist are skipped). */
+MLRA_API size_t mlra_mx4_pre_attention_workspace_bytes(int32_t batch, int32_t d, int32_t d_cq, int32_t n_blocks, int32_t d_cb,
+                                              int32_t d_r, int32_t h, int32_t d_h, int32_t dtype);
+MLRA_API int mlra_mx4_pre_attention(const mlra_mx4_cache* cache, const mlra_pre_weights* weights, int32_t batch,
+                           const void* hidden, const int32_t* positions, void* q_nope, void* q_rope, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 /* Bytes of workspace for mlra_mx4_decode_attn on the current device (0 on invalid sizes); h is the total number of heads. */
 MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, int32_t groups, int32_t n_blocks,
                                        int32_t d_cb, int32_t page_size, int32_t max_pages_per_seq);

@@ -25,6 +25,7 @@ EXPORTS = ("mlra_strerror", "mlra_append_kv", "mlra_absorb_q", "mlra_absorb_q_fo
            "mlra2_decode_attn", "mlra_decode_attn_gated", "mlra_decode_multi_workspace_bytes", "mlra_decode_attn_multi",
            "mlra_pre_attention_workspace_bytes", "mlra_pre_attention",
            "mlra_mx4_append_kv", "mlra_mx4_read_kv", "mlra_mx4_decode_workspace_bytes", "mlra_mx4_decode_attn",
+           "mlra_mx4_pre_attention_workspace_bytes", "mlra_mx4_pre_attention",
            "gqa_decode_workspace_bytes", "gqa_decode_attn", "mlra_kernel_timing_begin",
            "mlra_kernel_timing_end", "mlra_decode_plan_info", "mlra_decode_route_info", "mlra_probe_stream_read", "mlra_probe_shader_clock")
 
@@ -105,6 +106,10 @@ def load_library() -> ctypes.CDLL:
     lib.mlra_mx4_append_kv.argtypes = [mp, i32, i32, vp, vp, i32, vp, vp, vp]
     lib.mlra_mx4_read_kv.restype = ctypes.c_int
     lib.mlra_mx4_read_kv.argtypes = [mp, i32, i32, vp, vp, vp, vp, i32, vp]
+    lib.mlra_mx4_pre_attention_workspace_bytes.restype = sz
+    lib.mlra_mx4_pre_attention_workspace_bytes.argtypes = lib.mlra_pre_attention_workspace_bytes.argtypes
+    lib.mlra_mx4_pre_attention.restype = ctypes.c_int
+    lib.mlra_mx4_pre_attention.argtypes = [mp, ctypes.POINTER(_PreWeightsStruct), i32, vp, vp, vp, vp, vp, sz, vp]
     lib.mlra_mx4_decode_workspace_bytes.restype = sz
     lib.mlra_mx4_decode_workspace_bytes.argtypes = [i32] * 8
     lib.mlra_mx4_decode_attn.restype = ctypes.c_int
@@ -522,6 +527,33 @@ def mlra_mx4_read_kv(cache: Mx4Cache, positions: torch.Tensor, row_lens: Optiona
     _check(load_library().mlra_mx4_read_kv(ctypes.byref(cs), batch, n_rows, _ptr(positions), _ptr(row_lens), _ptr(c_kv_out),
                                            _ptr(k_rope_out), _dt(c_kv_out.dtype), _stream(stream)), "mlra_mx4_read_kv")
     return c_kv_out, k_rope_out
+
+
+def mlra_mx4_pre_attention_workspace_bytes(batch, d, d_cq, n_blocks, d_cb, d_r, h, d_h, dtype) -> int:
+    return int(load_library().mlra_mx4_pre_attention_workspace_bytes(batch, d, d_cq, n_blocks, d_cb, d_r, h, d_h, _dt(dtype)))
+
+
+def mlra_mx4_pre_attention(cache: Mx4Cache, weights: "PreWeights", hidden: torch.Tensor, positions: torch.Tensor,
+                           q_nope: Optional[torch.Tensor] = None, q_rope: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """mlra_pre_attention for a cache in 4 bits: stores the new token's row of every sequence, returns (q_nope, q_rope)."""
+    cs, ws = cache.struct(), weights.struct()
+    batch, d = hidden.shape
+    assert d == ws.d and hidden.dtype == weights.w_dq.dtype and positions.dtype == torch.int32
+    assert positions.shape == (batch,) and cache.page_table.shape[0] == batch
+    assert weights.w_dkv.shape[1] == cs.n_blocks * cs.d_cb and weights.w_kr.shape[1] == cs.d_r
+    if q_nope is None:
+        q_nope = torch.empty((batch, ws.h, ws.d_h), dtype=hidden.dtype, device=hidden.device)
+    if q_rope is None:
+        q_rope = torch.empty((batch, ws.h, cs.d_r), dtype=hidden.dtype, device=hidden.device)
+    if workspace is None:
+        need = mlra_mx4_pre_attention_workspace_bytes(batch, d, ws.d_cq, cs.n_blocks, cs.d_cb, cs.d_r, ws.h, ws.d_h, hidden.dtype)
+        workspace = torch.empty(need, dtype=torch.uint8, device=hidden.device)
+    _check(load_library().mlra_mx4_pre_attention(ctypes.byref(cs), ctypes.byref(ws), batch, _ptr(hidden), _ptr(positions),
+                                                 _ptr(q_nope), _ptr(q_rope), _ptr(workspace),
+                                                 workspace.numel() * workspace.element_size(), _stream(stream)),
+           "mlra_mx4_pre_attention")
+    return q_nope, q_rope
 
 
 def mlra_mx4_decode_workspace_bytes(batch: int, q_len: int, h: int, groups: int, n_blocks: int, d_cb: int, page_size: int,

@@ -346,6 +346,11 @@ using namespace mlra;
 
 extern "C" {
 
+// (c->page_table NULL: the rows themselves, see launch_pre_attention)
+static int pre_attention_common(const mlra_cache* c, const mlra_pre_weights* w, int32_t batch, const void* hidden,
+                                const int32_t* positions, void* q_nope, void* q_rope, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 int mlra_mx4_append_kv(const mlra_mx4_cache* c, int32_t batch, int32_t n_rows, const void* c_kv, const void* k_rope,
                        int32_t src_dtype, const int32_t* positions, const int32_t* row_lens, void* stream) {
   const int st = mx4_rows_common(c, batch, n_rows, c_kv, k_rope, src_dtype, positions);
@@ -358,6 +363,44 @@ int mlra_mx4_read_kv(const mlra_mx4_cache* c, int32_t batch, int32_t n_rows, con
   const int st = mx4_rows_common(c, batch, n_rows, c_kv_out, k_rope_out, dst_dtype, positions);
   if (st != MLRA_OK) return st;
   return launch_mx4_read(c, batch, n_rows, positions, row_lens, c_kv_out, k_rope_out, dst_dtype, (hipStream_t)stream);
+}
+
+// (behind the workspace of the projections: the new rows, fp32)
+static size_t mx4_rows_bytes(int batch, int width) { return align_up((size_t)batch * width * sizeof(float), 256); }
+
+size_t mlra_mx4_pre_attention_workspace_bytes(int32_t batch, int32_t d, int32_t d_cq, int32_t n_blocks, int32_t d_cb,
+                                              int32_t d_r, int32_t h, int32_t d_h, int32_t dtype) {
+  const size_t need = mlra_pre_attention_workspace_bytes(batch, d, d_cq, n_blocks, d_cb, d_r, h, d_h, dtype);
+  if (need == 0 || d_cb % 32 != 0) return 0;
+  return align_up(need, 256) + mx4_rows_bytes(batch, n_blocks * d_cb) + mx4_rows_bytes(batch, d_r);
+}
+
+int mlra_mx4_pre_attention(const mlra_mx4_cache* c, const mlra_pre_weights* w, int32_t batch, const void* hidden,
+                           const int32_t* positions, void* q_nope, void* q_rope, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  if (!c || !w || !hidden || !positions || !q_nope || !q_rope) return MLRA_ERR_NULL;
+  if (!c->latent || !c->scales || !c->rope || !c->page_table) return MLRA_ERR_NULL;
+  const int bad = check_mx4_cache(c, batch);
+  if (bad != MLRA_OK) return bad;
+  if (!valid_dtype(w->dtype)) return MLRA_ERR_DTYPE;
+  const size_t pre = mlra_pre_attention_workspace_bytes(batch, w->d, w->d_cq, c->n_blocks, c->d_cb, c->d_r, w->h, w->d_h, w->dtype);
+  if (pre == 0) return MLRA_ERR_SHAPE;
+  const size_t need = mlra_mx4_pre_attention_workspace_bytes(batch, w->d, w->d_cq, c->n_blocks, c->d_cb, c->d_r, w->h, w->d_h,
+                                                             w->dtype);
+  if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 256 != 0) return MLRA_ERR_WORKSPACE;
+  // the rows as pages of one token, in fp32, so that a latent is rounded once
+  mlra_cache rows = {};
+  rows.latent = (char*)workspace + align_up(pre, 256);
+  rows.rope = (char*)rows.latent + mx4_rows_bytes(batch, c->n_blocks * c->d_cb);
+  rows.num_pages = batch;
+  rows.page_size = rows.max_pages_per_seq = 1;
+  rows.n_blocks = c->n_blocks;
+  rows.d_cb = c->d_cb;
+  rows.d_r = c->d_r;
+  rows.dtype = MLRA_F32;
+  const int st = pre_attention_common(&rows, w, batch, hidden, positions, q_nope, q_rope, workspace, pre, stream);
+  if (st != MLRA_OK) return st;
+  return launch_mx4_append(c, batch, 1, rows.latent, rows.rope, MLRA_F32, positions, nullptr, (hipStream_t)stream);
 }
 
 size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, int32_t h, int32_t groups, int32_t n_blocks,
@@ -608,6 +651,12 @@ int mlra_pre_attention(const mlra_cache* c, const mlra_pre_weights* w, int32_t b
                        size_t workspace_bytes, void* stream) {
   if (!c || !w || !hidden || !positions || !q_nope || !q_rope) return MLRA_ERR_NULL;
   if (!c->latent || !c->rope || !c->page_table) return MLRA_ERR_NULL;
+  return pre_attention_common(c, w, batch, hidden, positions, q_nope, q_rope, workspace, workspace_bytes, stream);
+}
+
+static int pre_attention_common(const mlra_cache* c, const mlra_pre_weights* w, int32_t batch, const void* hidden,
+                                const int32_t* positions, void* q_nope, void* q_rope, void* workspace,
+                                size_t workspace_bytes, void* stream) {
   if (!w->w_dq || !w->w_dkv || !w->w_kr || !w->w_uq || !w->w_qr) return MLRA_ERR_NULL;
   if (!valid_dtype(c->dtype) || !valid_dtype(w->dtype)) return MLRA_ERR_DTYPE;
   if (batch <= 0 || batch > 65535 || w->d <= 0 || w->d_cq <= 0 || w->h <= 0 || w->d_h <= 0 || c->n_blocks <= 0 ||

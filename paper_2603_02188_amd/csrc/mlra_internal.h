@@ -208,6 +208,7 @@ struct PrePlan {
   size_t off_part1, off_cq, off_cs, off_part2, bytes;   // workspace layout
 };
 PrePlan pre_plan(int dtype, int batch, int d, int d_cq, int d_c, int d_r, int h, int d_h);
+// (c->page_table NULL: the new rows go to pages of one token, row s to page s, for whoever wants the rows themselves)
 int launch_pre_attention(const mlra_cache* c, const mlra_pre_weights* w, int batch, const void* hidden,
                          const int32_t* positions, void* q_nope, void* q_rope, void* workspace,
                          hipStream_t stream);

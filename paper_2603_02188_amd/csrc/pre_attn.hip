@@ -281,7 +281,8 @@ __global__ __launch_bounds__(kFinishThreads) void pre_finish_down_kernel(
   const int c0 = kv ? d_cq : 0, n_norm = kv ? d_c : d_cq, nc = kv ? d_c + d_r : d_cq;
   const T* const gain = kv ? gain_kv : gain_q;
   const int pos = positions[s];
-  const int page = kv && pos >= 0 ? page_table[(size_t)s * max_pages + pos / page_size] : 0;
+  // (no page table: the rows themselves are wanted, row s in page s of one token)
+  const int page = kv && pos >= 0 ? (page_table ? page_table[(size_t)s * max_pages + pos / page_size] : s) : 0;
   // gains of the columns that this thread finishes (the later ones of rows beyond four rounds are fetched when they are
   // used); they go on last, so that a column times its gain stays in range where the result does
   constexpr int kGains = 4;
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(kFinishThreads) void pre_finish_down_kernel(
     return;
   }
   if (pos < 0) return;                        // no cache row for this sequence (as in mlra_append_kv)
-  const int slot = pos % page_size;
+  const int slot = page_table ? pos % page_size : 0;
   const int d_cb = d_c / n_blocks;
   each([&](int j, float v) {
     const int b = j / d_cb, c = j % d_cb;

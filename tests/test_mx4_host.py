@@ -125,3 +125,25 @@ def test_binding_checks_shapes():
         args.update(bad)
         with pytest.raises((AssertionError, ValueError)):
             mlra.Mx4Cache(**args).struct()
+
+
+def test_bad_pre_attention_calls_are_refused():
+    lib, cs = mlra.load_library(), _struct()
+    pw = lambda **kw: mlra._PreWeightsStruct(*{**dict(w_dq=256, w_dkv=256, w_kr=256, w_uq=256, w_qr=256, gain_q=None, gain_kv=None, d=96,
+                                                      d_cq=40, h=8, d_h=64, dtype=1, alpha_q=1.0, alpha_kv=1.0, eps=1e-6,
+                                                      rope_base=1e4), **kw}.values())
+
+    def call(c, w, batch=2, hidden=_ONE, pos=_ONE, ws=_ONE, ws_bytes=1 << 30):
+        return lib.mlra_mx4_pre_attention(c and ctypes.byref(c), w and ctypes.byref(w), batch, hidden, pos, _ONE, _ONE, ws, ws_bytes,
+                                          _NULL)
+
+    assert call(None, pw()) == call(cs, None) == call(cs, pw(), hidden=_NULL) == call(cs, pw(), pos=_NULL) == -1
+    assert call(cs, pw(w_dq=None)) == -1
+    assert call(cs, pw(dtype=9)) == -3
+    assert call(cs, pw(), batch=0) == call(cs, pw(d=0)) == call(cs, pw(d_h=63)) == call(_struct(d_r=31), pw()) == -2
+    assert call(cs, pw(), ws=_NULL) == call(cs, pw(), ws_bytes=16) == call(cs, pw(), ws=264) == -4
+    size = mlra.mlra_mx4_pre_attention_workspace_bytes
+    assert size(2, 96, 40, 4, 64, 32, 8, 64, torch.float32) >= 2 * (256 + 32) * 4
+    assert size(2, 96, 40, 4, 48, 32, 8, 64, torch.float32) == size(0, 96, 40, 4, 64, 32, 8, 64, torch.float32) == 0
+    for kw, status in _BAD_CACHE:
+        assert call(_struct(**kw), pw()) == status, kw
