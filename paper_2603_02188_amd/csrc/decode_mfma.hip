@@ -34,7 +34,7 @@
 //
 // MX4, for the latent cache in 4 bits (plain and PAIRED form): the stages hold the codes and scales as they lie in memory
 // (13 or 17 KiB).  The scores take them as they are: v_mfma_scale_f32_32x32x64_f8f6f4 multiplies E2M1 codes, scaled by group,
-// with E2M3 numbers at four times the rate of bf16, and a query is the sum of two of those (see the prologue), so that the
+// with E2M3 numbers at four times the rate of bf16, and a query is the sum of two of those, or three (mx4_tile.h), so that the
 // latent channels cost half of what they do in bf16.  The RoPE channels stay bf16.  For the values, whose scales run along the
 // wrong axis for that instruction (a scale per token, which is the k index there), two tiles are widened to bf16, which is
 // exact: each wave widens the 16 rows that it loaded itself, tile j + 2 behind the value MFMAs of step j, into the place of
@@ -797,8 +797,10 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 
   // ---- prologue: every stage gets a tile; scores and column maxima of tile 0; K operands of tile 1 ----
   bf16x8 qreg[2][12];
-  u32x6 qmx[2][2][2];           // (MX4) [head tile][64 channels][term]
-  unsigned qmx_sc[2] = {0, 0};  // ... and their scales, byte 2 ks + term
+  u32x6 qmx[2][2][3];           // (MX4) [head tile][64 channels][term]
+  unsigned qmx_sc[2] = {0, 0};  // ... and their scales, byte 2 ks + term, of the third term byte 2 ks
+  unsigned qmx_sc3[2] = {0, 0};
+  bool third = false;           // a group of these queries wants its third term
   issue_last_tile();
   for (int jj = 1; jj < STAGES - kQStages && jj < ntiles; ++jj) issue_tile();
   if (GLA && tid < 4) ((float*)(smem + STAGES * kStageB))[tid] = 0.f;   // the zeros some RoPE reads below take
@@ -834,11 +836,15 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[8 * i + e] = (float)part[e] * sc;
         }
-        u32x6 hi, lo;
-        qmx_sc[nt] |= mx4_tile::split_query(v, hi, lo) << (16 * ks);
-        asm volatile("" : "+a"(hi), "+a"(lo));
-        qmx[nt][ks][0] = hi;
-        qmx[nt][ks][1] = lo;
+        u32x6 rows[3];
+        const unsigned bytes = mx4_tile::split_query(v, rows, third);
+        qmx_sc[nt] |= (bytes & 0xffffu) << (16 * ks);
+        qmx_sc3[nt] |= (bytes >> 16) << (16 * ks);
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          asm volatile("" : "+a"(rows[t]));
+          qmx[nt][ks][t] = rows[t];
+        }
       }
     }
     constexpr int kFirst = MX4 ? 8 : 0;
@@ -883,10 +889,11 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-          for (int term = 0; term < 2; ++term) {
+          for (int term = 0; term < 3; ++term) {
             f32x16& acc = nt == 0 ? sa0 : sa1;
+            const unsigned sc_q = term == 2 ? qmx_sc3[nt] >> (16 * ks) : qmx_sc[nt] >> (16 * ks + 8 * term);
             acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kt, mx4_tile::operand(qmx[nt][ks][term]), acc, 4, 2, 0,
-                                                                  ksc >> (16 * ks), 0, qmx_sc[nt] >> (16 * ks + 8 * term));
+                                                                  ksc >> (16 * ks), 0, sc_q);
           }
       }
     }
@@ -954,6 +961,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // codes are widened and its RoPE rows were read in the previous step, and takes tile j + 1 + STAGES; tile STAGES goes out
   // here.)
   unsigned st_cur = 0, ring_cur = 0;
+  const bool third_any = MX4 && __any(third);
   if (MX4) {
     wait_vm_lgkm<63>();
     __builtin_amdgcn_s_barrier();
@@ -988,7 +996,13 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         else if (i < 8) score_mx(acc, ks, term, qmx[nt][ks][term], qmx_sc[nt]);
         else score_mfma(acc, ka[8 + ((i - 8) >> 1)], qreg[nt][8 + ((i - 8) >> 1)]);
         if (i == 3) { hold(va[1][2]); hold(va[1][3]); hold(pb0[1]); hold(pb1[1]); }
-        if (i == 8) hold_raw(kraw[0]);
+        if (i == 7 && __builtin_expect(third_any, 0)) {
+          score_mx(n0, 0, 0, qmx[0][0][2], qmx_sc3[0]);
+          score_mx(n1, 0, 0, qmx[1][0][2], qmx_sc3[1]);
+          score_mx(n0, 1, 0, qmx[0][1][2], qmx_sc3[0]);
+          score_mx(n1, 1, 0, qmx[1][1][2], qmx_sc3[1]);
+        }
+        if (i == 11) hold_raw(kraw[0]);
         if (i == 12) { hold_raw(kraw[1]); asm volatile("" : : "v"(ksc)); }
         if (i == 14) hold(ka[8]);
         if (i < 8) prob_exp(c0, 2 * i, pr[2 * (i & 1)], pr[2 * (i & 1) + 1]);

@@ -428,13 +428,14 @@ constexpr int kPPOff = kPStages * kMStage, kPAOff = kPPOff + 2 * kMPBytes, kPXOf
               kPFOff = kPXOff + 2 * 4 * 32 * 4, kPLds = kPFOff + 2 * 4 * 4;
 static_assert(kPLds <= 160 * 1024, "one workgroup per CU");
 // Latent cache in 4 bits: the stages hold codes, scales (1 KiB) and RoPE rows as they lie in memory, 13 KiB.  The scores take the
-// codes as they are (v_mfma_scale_f32_16x16x128_f8f6f4, the queries as sums of two E2M3 numbers: see decode_mfma.hip); for the
+// codes as they are (v_mfma_scale_f32_16x16x128_f8f6f4, the queries as sums of two or three E2M3 numbers: see mx4_tile.h); for the
 // value product two tiles, behind what is above, hold the latent channels widened to bf16.  A wave widens the eight rows that it
 // loaded itself: read behind the value product of step j, tile j + 2 is converted and written during the scores of step j + 1.
 constexpr int kXRow = kMDc / 2, kXScaleRow = kMDc / mx4_tile::kGroup, kXScales = kMTok * kXRow, kXRope = kXScales + 1024,
               kXStage = kXRope + kMRopeBytes, kXLoads = 4;
 constexpr int kXRing = kPStages * kXStage, kXShift = kXRing + 2 * kMLatBytes - kPPOff;   // (the tables move up by kXShift)
-constexpr int kXLds = kPLds + kXShift;
+constexpr int kXThird = kPLds + kXShift;       // third rows of the queries, 12 KiB for 32 heads, which few launches read
+constexpr int kXThirdBytes = 8 * 64 * 24, kXLds = kXThird + 2 * kXThirdBytes;
 static_assert(kXLds <= 160 * 1024, "one workgroup per CU");
 
 template <bool MX4>
@@ -544,6 +545,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   // ---- query operands of this wave's 32 heads, two groups of 16
   bf16x8 qreg[2][18];
   mx4_tile::u32x6 qmx[2][4][2];    // (4 bits) [group][128 channels][term], a lane's 32 channels are one group of the cache's side
+  bool third = false;
   unsigned qmx_sc[2][4] = {};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -560,7 +562,15 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[8 * e8 + e] = (float)part[e];
         }
-        qmx_sc[i][ks] = mx4_tile::split_query(v, qmx[i][ks][0], qmx[i][ks][1]);
+        mx4_tile::u32x6 rows[3];
+        qmx_sc[i][ks] = mx4_tile::split_query(v, rows, third);
+        qmx[i][ks][0] = rows[0];
+        qmx[i][ks][1] = rows[1];
+        if (th == 0) {               // (both waves of these heads have the same)
+          unsigned char* const at = smem + kXThird + hg * kXThirdBytes;
+          *(mx4_tile::u32x4*)(at + ((4 * i + ks) * 64 + lane) * 16) = mx4_tile::u32x4{rows[2][0], rows[2][1], rows[2][2], rows[2][3]};
+          *(uint2*)(at + 8 * 64 * 16 + ((4 * i + ks) * 64 + lane) * 8) = make_uint2(rows[2][4], rows[2][5]);
+        }
       }
     } else {
 #pragma unroll
@@ -666,6 +676,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     typedef __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
     *(u32x4_ptr)(size_t)((lat + wd_out[r]) ^ (i << 4)) = mx4_tile::decode8(wd_raw[r][i], mx4_tile::scale_of(wd_byte[r]));
   };
+  const bool third_any = MX4 && __any(third);
   // scores of a tile whose operands are read, with the operands of the value product of the tile before it and (with_v) the tile
   // itself widened into wl
   auto scores_mx4 = [&](unsigned vb, int par, auto with_v, unsigned wl) {
@@ -673,6 +684,20 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     s[0] = s[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) kx_sc[i] >>= 8 * q4;       // group 4 ks + q4 in byte 0
+    if (__builtin_expect(third_any, 0)) {
+      const unsigned char* const at = smem + kXThird + hg * kXThirdBytes;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const mx4_tile::u32x4 lo = *(const mx4_tile::u32x4*)(at + ((4 * i + ks) * 64 + lane) * 16);
+          const uint2 hi = *(const uint2*)(at + 8 * 64 * 16 + ((4 * i + ks) * 64 + lane) * 8);
+          const mx4_tile::u32x6 row = {lo[0], lo[1], lo[2], lo[3], hi.x, hi.y};
+          s[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_tile::operand(kx[ks]), mx4_tile::operand(row), s[i], 4, 2, 0,
+                                                                  kx_sc[ks], 2, qmx_sc[i][ks]);
+          __builtin_amdgcn_sched_barrier(0);   // (one row in registers at a time)
+        }
+    }
 #pragma unroll
     for (int m = 0; m < 10; ++m) {
 #pragma unroll

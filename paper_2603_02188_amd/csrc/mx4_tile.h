@@ -44,29 +44,42 @@ __device__ __forceinline__ u32x4 decode8(unsigned codes, float scale) {
                __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 
-// 32 query channels, one group of the cache's side, as the sum of two rows of E2M3 numbers (four significant bits, up to 7.5)
-// with a power of two each, 2^-5 apart, for v_mfma_scale_f32_*_f8f6f4.  What is left is 2^-10 of the largest channel at most,
-// less than bf16 leaves of a query in the mean (0.11 % against 0.165 %).  The first row takes the next power of two from 1.875
-// 2^e on; a group with an infinity or a NaN is NaN.  Returns the scale bytes, hi | lo << 8.
+// 32 query channels, one group of the cache's side, as the sum of rows of E2M3 numbers (four significant bits, up to 7.5) with a
+// power of two each, 2^-5 apart, for v_mfma_scale_f32_*_f8f6f4.  Two rows leave 2^-10 of the largest channel at most, on normal
+// channels less than bf16 leaves of a query in the mean (0.11 % against 0.165 %).  That is no longer so where a channel is far
+// above the rest, which the two rows round as coarsely as it: if the largest is more than eight times the mean magnitude, a
+// third row is wanted, after which 2^-15 of it is left.  The first row takes the next power of two from 1.875 2^e on; a group
+// with an infinity or a NaN is NaN.  Returns the scale bytes, hi | lo << 8 | third << 16.
 typedef __attribute__((ext_vector_type(6))) unsigned u32x6;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
 typedef __attribute__((ext_vector_type(32))) float f32x32;
-__device__ __forceinline__ unsigned split_query(const f32x32& v, u32x6& hi, u32x6& lo) {
-  unsigned top = 0;
-#pragma unroll
-  for (int e = 0; e < 32; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-  const int ex = min(max((int)((top + 0x100000u) >> 23) - 2, 7), 252);
-  const float s_hi = __uint_as_float((unsigned)ex << 23), s_lo = __uint_as_float((unsigned)(ex - 5) << 23);
+__device__ __forceinline__ u32x6 query_row(const f32x32& v, float scale) {
   bf16x32 x;
 #pragma unroll
   for (int e = 0; e < 32; ++e) x[e] = (__bf16)v[e];
-  hi = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, s_hi);
-  const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(hi, s_hi);
+  return __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale);
+}
+__device__ __forceinline__ unsigned split_query(f32x32 v, u32x6 (&rows)[3], bool& third) {
+  float top = 0.f, sum = 0.f;
 #pragma unroll
-  for (int e = 0; e < 32; ++e) x[e] = (__bf16)(v[e] - back[e]);
-  lo = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, s_lo);
-  return top < 0x7f800000u ? (unsigned)ex | (unsigned)(ex - 5) << 8 : 0xffffu;
+  for (int e = 0; e < 32; ++e) {
+    top = fmaxf(top, fabsf(v[e]));
+    sum += fabsf(v[e]);
+  }
+  const bool wanted = 4.f * top > sum, finite = sum < INFINITY;   // (a NaN is in the sum)
+  third |= wanted;
+  const int ex = min(max((int)((__float_as_uint(top) + 0x100000u) >> 23) - 2, 12), 252);
+  auto scale = [&](int t) { return __uint_as_float((unsigned)(ex - 5 * t) << 23); };
+  rows[0] = query_row(v, scale(0));
+  v -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(rows[0], scale(0));
+  rows[1] = query_row(v, scale(1));
+  rows[2] = u32x6{0u, 0u, 0u, 0u, 0u, 0u};
+  if (__any(wanted)) {       // (a wave whose groups all do without skips it: a group that it may use has it or zeros)
+    v -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(rows[1], scale(1));
+    rows[2] = query_row(v, scale(2));
+  }
+  return finite ? (unsigned)ex | (unsigned)(ex - 5) << 8 | (unsigned)(ex - 10) << 16 : 0xffffffu;
 }
 
 // Operands of the builtin, whose registers behind the format's are not read

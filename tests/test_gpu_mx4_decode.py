@@ -164,6 +164,67 @@ def test_scores_of_any_size(dtype):
         assert np.abs(got).max() <= 4.0 * np.abs(ref).max()
 
 
+# one query channel far above its group's others, against cached channels that are small there: what the others contribute is
+# then most of a score, and has to keep its precision.  (Bars as above: 1e-2 of the largest output.  32 channels with the scale's
+# power of two cut to 1/64 in one of them: scores stay as they are.)
+@pytest.mark.parametrize("n_blocks,d_cb,h,factor", [(4, 128, 128, 12.0), (4, 128, 128, 64.0), (4, 128, 64, 200.0), (1, 512, 128, 64.0),
+                                                    (1, 512, 20, 200.0), (2, 64, 16, 64.0)])
+def test_query_channels_that_stand_out(n_blocks, d_cb, h, factor):
+    lens, tau = [500, 65, 3], 1.0 / np.sqrt(192)
+    hc = HostCache(lens, n_blocks, d_cb, 64, "bf16", 64, 21)
+    hc.latent[:, :, :, 3::16] &= 0xF0                            # (the channel of the large query holds zeros)
+    hc.rows = [np.where(np.arange(d_cb) % 32 == 6, 0.0, r) for r in hc.rows]
+    rng = np.random.default_rng(22)
+    (qa, qa64), (qr, qr64), (wv, wv64) = queries(rng, 3, 1, n_blocks, h, 1, d_cb, 64, 128, "bf16")
+    qa64[..., 6::32] *= factor
+    qa, qa64 = stored(qa64, "bf16")
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, tau, out_dtype=torch.float32).double().cpu().numpy()
+    ref, _ = orc.attend(hc.rows, hc.ropes, lens, qa64, qr64, wv64, tau)
+    err = max_rel_err(got, ref)
+    print(f"       max rel err {err:.3e}", flush=True)
+    assert err <= 1e-2
+
+
+@pytest.mark.parametrize("n_blocks,d_cb,h", [(4, 128, 128), (4, 128, 64), (1, 512, 64)])
+def test_nan_and_infinite_queries_and_rows_of_the_pipelined_kernels(n_blocks, d_cb, h):
+    """A NaN or an infinity in a query reaches its head, one in a row its sequence, and neither another sequence.  (The row sums
+    of heads 16 apart come from one matrix product over both, as on the wider caches, so that these two go together.)"""
+    lens = [200, 130, 64]
+    hc = HostCache(lens, n_blocks, d_cb, 64, "bf16", 64, 23)
+    rng = np.random.default_rng(24)
+    (qa, qa64), (qr, _), (wv, _) = queries(rng, 3, 1, n_blocks, h, 1, d_cb, 64, 128, "bf16")
+    want = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, 0.07)
+    bad = qa.clone()
+    bad[0, 0, 0, 5, 40], bad[1, 0, 0, 7, 1] = float("nan"), float("inf")
+    got = mlra.mlra_mx4_decode_attn(hc.device(), bad, qr, wv, 0.07)
+    assert got[0, 0, 5].isnan().all() and got[1, 0, 7].isnan().all() and torch.equal(got[2], want[2])
+    others = [i for i in range(h) if i % 32 not in (5, 21, 7, 23)]
+    assert torch.equal(got[:, :, others], want[:, :, others])
+    hc.scales[hc.table[1, 2], 0, 1, 2] = 255                     # the last row of sequence 1
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, 0.07)
+    assert got[1].isnan().all() and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("n_blocks,d_cb,dtype", [(4, 128, "bf16"), (1, 512, "bf16"), (4, 128, "f32")])
+def test_pages_beyond_4_gib(n_blocks, d_cb, dtype):
+    """The same rows in the first pages of a pool and in pages whose codes lie behind 2^32 bytes."""
+    page, pages = 64, (1 << 32) // (64 * 256) + 40
+    lens = torch.tensor([150, 64], dtype=torch.int32, device="cuda")
+    rng = np.random.default_rng(30)
+    (qa, _), (qr, _), (wv, _) = queries(rng, 2, 1, n_blocks, 64, 1, d_cb, 64, 32, dtype)
+    g = torch.Generator("cuda").manual_seed(2)
+    rows, rope = torch.randn((2, 150, 512), generator=g, device="cuda"), torch.randn((2, 150, 64), generator=g, device="cuda")
+    cache = mlra.Mx4Cache.empty(pages, n_blocks, page, d_cb, 64, torch.zeros((2, 3), dtype=torch.int32, device="cuda"), lens,
+                                torch.bfloat16 if dtype == "bf16" else torch.float32)
+    outs = []
+    for first in (0, pages - 6):
+        cache.page_table = torch.arange(first, first + 6, dtype=torch.int32, device="cuda").view(2, 3)
+        mlra.mlra_mx4_append_kv(cache, rows, rope, torch.zeros_like(lens), lens)
+        outs.append(mlra.mlra_mx4_decode_attn(cache, qa, qr, wv, 0.07))
+        cache.latent[:6], cache.scales[:6] = 0, 255
+    assert outs[0].isfinite().all() and torch.equal(outs[0], outs[1])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_nan_rows_reach_their_sequence_only(dtype):
     lens = [100, 80]
