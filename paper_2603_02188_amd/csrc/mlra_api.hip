@@ -156,7 +156,7 @@ struct Route {
 // 32 heads, whole steps: 100 sequences of 8000 tokens 64 us against 87, 4 of 8192 26 against 30; 48 heads 80 and 88, 30 and 30,
 // 16 of 16K 44 and 42).
 static bool mx4_pipelined(const DecodeArgs& a) {
-  return (decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a);
+  return !a.precise && ((decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a));
 }
 
 // Which kernels a call takes, from its shape; sets a.fitted and a.fit_tiles.
@@ -173,7 +173,7 @@ static Route choose_route(DecodeArgs& a) {
              : decode_gla_supported(a) ? kGla
              : decode_f32_supported(a) ? kF32
                                        : kPlain;
-  r.merge_mfma = merge_upproj_mfma_supported(a);
+  r.merge_mfma = merge_upproj_mfma_supported(a) && !(a.precise && a.out_dtype == MLRA_F32);
   a.fitted = r.kernel == kMlra ? r.merge_mfma && a.batch / a.q_group <= 64 &&
                                      (a.q_group > 1 || (a.plan.target_chunks > 0 && !a.plan.single_if_uniform))
              : r.kernel == kMla ? mla_mfma_fits_chunks(a)
@@ -461,6 +461,7 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   a.stream = (hipStream_t)stream;
   a.t_main = timing_pair(0);
   a.t_epi = timing_pair(1);
+  a.precise = c->dtype == MLRA_BF16 && (out_dtype == MLRA_F32 || lse);
   if (!mx4_pipelined(a)) a.plan = plan_mx4(units, hb, c->n_blocks, c->d_cb, c->dtype, max_seq_len, a.cus);
   int32_t* const lens = (int32_t*)workspace;
   int32_t* const table = (int32_t*)((char*)workspace + align_up((size_t)units * sizeof(int32_t), 256));

@@ -116,6 +116,7 @@ struct DecodeArgs {
   int dtype;
   hipStream_t stream;
   KernelTimer t_main, t_epi;   // set by mlra_kernel_timing_begin: the decode kernel and the merge / up-projection
+  bool precise = false;   // (4 bits, bf16) an output is fp32, and exact to it
   const void* scales = nullptr;   // of a latent cache in 4 bits ([num_pages][n_blocks][page_size][d_cb / 32]); null: none
 };
 

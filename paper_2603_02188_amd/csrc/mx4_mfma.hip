@@ -11,6 +11,9 @@
 //     probability is the sum of three bf16 numbers (24 bits), a product with the latents three matrix instructions; the RoPE
 //     part, fp32 on both sides, takes the six products of terms down to 2^-24.  (The fp32 matrix instructions have a
 //     sixteenth of the rate.)
+//   * fp32 outputs of a bf16 call (the output itself, or the log-sum-exp) are exact to fp32: cache, queries and weights are exact
+//     in bf16 as they come, so that only the probabilities, as three bf16 numbers (two, 2^-17, if the log-sum-exp alone is fp32),
+//     and the merge, on the fp32 matrix instructions, differ from a bf16 output's.
 //   * the running maximum moves only when a tile outgrows it by more than 2^8; (m, l, Z) is consistent for any reference.
 //   * rows are 16 bytes longer than their channels, so that sixteen rows start in sixteen different bank groups.
 #include "f32_tile.h"
@@ -75,7 +78,8 @@ __device__ __forceinline__ short4v read_tr16(const __bf16* p) {
 }
 
 // DP, RP: latent and RoPE channels of the tile, at least d_cb and d_r; VEC: RoPE rows and queries in pieces of four elements
-template <typename T, int DP, int RP, int NH, bool VEC>
+// PT: bf16 terms of a probability
+template <typename T, int DP, int RP, int NH, bool VEC, int PT>
 __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
   typedef typename RawOf<T>::type Raw;
   constexpr int N = Terms<T>::n;
@@ -282,17 +286,22 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
     const int valid = t1 - t0 - j * kTile - tok0;       // tokens of this wave's share that exist
     float mx[NH], lowest = INFINITY;
     bool grown = false;
+    if (valid < 32) {                   // (uniform: the chunk's last tile)
+#pragma unroll
+      for (int m = 0; m < NH; ++m)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[m][tt][i] = 16 * tt + 4 * q + i < valid ? sc[m][tt][i] : -INFINITY;
+    }
 #pragma unroll
     for (int m = 0; m < NH; ++m) {
       mx[m] = -INFINITY;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = sc[m][tt][i] * p.scale_log2;
-          sc[m][tt][i] = 16 * tt + 4 * q + i < valid ? x : -INFINITY;
-          mx[m] = fmaxf(mx[m], sc[m][tt][i]);
-        }
+        for (int i = 0; i < 4; ++i) mx[m] = fmaxf(mx[m], sc[m][tt][i]);
+      mx[m] *= p.scale_log2;
       mx[m] = fmaxf(mx[m], __shfl_xor(mx[m], 16));
       mx[m] = fmaxf(mx[m], __shfl_xor(mx[m], 32));
       grown |= mx[m] > m_run[m] + kLazy;
@@ -307,13 +316,13 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
         for (int ct = 0; ct < CT; ++ct) z[ct][m] *= alpha;
       }
     }
-    bf16x8 pb[NH][N];
+    bf16x8 pb[NH][PT];
 #pragma unroll
     for (int m = 0; m < NH; ++m) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[m][tt][i] -= m_run[m];
+        for (int i = 0; i < 4; ++i) sc[m][tt][i] = __builtin_fmaf(sc[m][tt][i], p.scale_log2, -m_run[m]);
       if constexpr (N > 1) {
         // (the exponential instruction returns zero below 2^-126, exp2f spends a few more on a denormal result: only where
         // there is one, the other bits are the same)
@@ -342,11 +351,11 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          __bf16 t[N];
+          __bf16 t[PT];
           split(sc[m][tt][i], t);
 #pragma unroll
-          for (int c = 0; c < N; ++c) pb[m][c][4 * tt + i] = t[c];
-          l_run[m] += N > 1 ? sc[m][tt][i] : (float)t[0];     // (bf16: over the weights that the values get)
+          for (int c = 0; c < PT; ++c) pb[m][c][4 * tt + i] = t[c];
+          l_run[m] += PT > 1 ? sc[m][tt][i] : (float)t[0];    // (one term: over the weights that the values get)
         }
     }
     const __bf16* const v0 = lat + (tok0 + 4 * q + (r16 >> 2)) * LP + 4 * (r16 & 3);
@@ -355,7 +364,7 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
       const short4v lo = read_tr16(v0 + 16 * ct), hi = read_tr16(v0 + 16 * LP + 16 * ct);
       const bf16x8 vt = __builtin_bit_cast(bf16x8, (short8v)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-      for (int c = 0; c < N; ++c)
+      for (int c = 0; c < PT; ++c)
 #pragma unroll
         for (int m = 0; m < NH; ++m) z[ct][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb[m][c], z[ct][m], 0, 0, 0);
     }
@@ -405,14 +414,14 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
   }
 }
 
-template <typename T, int DP, int RP, int NH, bool VEC>
-int launch_one(const DecodeArgs& a, Mx4Params& p) {
+template <typename T, int DP, int RP, int NH, bool VEC, int PT>
+int launch_terms(const DecodeArgs& a, Mx4Params& p) {
   constexpr size_t lds = lds_bytes<T, DP, RP, NH>();
   if (lds > 64 * 1024) {
     static PerDeviceSetup setup;
     int dev = -1;
     if (setup.needed(&dev)) {
-      if (hipFuncSetAttribute((const void*)mx4_decode_kernel<T, DP, RP, NH, VEC>,
+      if (hipFuncSetAttribute((const void*)mx4_decode_kernel<T, DP, RP, NH, VEC, PT>,
                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
         return MLRA_ERR_LAUNCH;
       setup.done(dev);
@@ -424,8 +433,16 @@ int launch_one(const DecodeArgs& a, Mx4Params& p) {
   constexpr long long kRow = 1 << 23;
   if (wgs > 0x7fffffffLL - kRow) return MLRA_ERR_LAUNCH;
   const dim3 grid((unsigned)(wgs < kRow ? wgs : kRow), (unsigned)((wgs + kRow - 1) / kRow));
-  mx4_decode_kernel<T, DP, RP, NH, VEC><<<grid, 256, lds, a.stream>>>(p);
+  mx4_decode_kernel<T, DP, RP, NH, VEC, PT><<<grid, 256, lds, a.stream>>>(p);
   return check_launch();
+}
+
+template <typename T, int DP, int RP, int NH, bool VEC>
+int launch_one(const DecodeArgs& a, Mx4Params& p) {
+  if constexpr (Terms<T>::n > 1) return launch_terms<T, DP, RP, NH, VEC, 3>(a, p);
+  else return !a.precise ? launch_terms<T, DP, RP, NH, VEC, 1>(a, p)
+              : a.out_dtype == MLRA_F32 ? launch_terms<T, DP, RP, NH, VEC, 3>(a, p)
+                                        : launch_terms<T, DP, RP, NH, VEC, 2>(a, p);
 }
 
 template <typename T, int DP, int RP, bool VEC>

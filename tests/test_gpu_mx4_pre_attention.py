@@ -65,7 +65,7 @@ def test_captured_step_from_hidden_states():
     pre_ws = torch.empty(mlra.mlra_mx4_pre_attention_workspace_bytes(3, 512, 128, 4, 128, 64, 128, 128, torch.bfloat16),
                          dtype=torch.uint8, device="cuda")
     qa, ws = torch.empty((3, 4, 128, 128), dtype=torch.bfloat16, device="cuda"), torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
-    out = torch.empty((3, 128, 128), dtype=torch.float32, device="cuda")
+    out = torch.empty((3, 128, 128), dtype=torch.bfloat16, device="cuda")
 
     def step():
         mlra.mlra_mx4_pre_attention(c, W, hidden, pos, qn, qr, pre_ws)
@@ -92,4 +92,4 @@ def test_captured_step_from_hidden_states():
     host = lambda t: t.double().cpu().numpy()
     ref, _ = mx4_oracle.attend([host(r).reshape(128, 4, 128) for r in rows], list(host(ropes)), lens.tolist(), host(qa)[:, None],
                                host(qr)[:, None], host(w_uv), wl.tau)
-    assert max_rel_err(host(out), ref[:, 0]) <= 1e-2
+    assert max_rel_err(host(out), ref[:, 0]) <= 1e-2 + 2.0 ** -8

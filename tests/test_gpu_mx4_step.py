@@ -77,8 +77,8 @@ def test_prompts_and_steps(dtype, groups, folded):
         else:
             qa = absorb(qn, loop.w_uk)
         out = mlra.mlra_mx4_decode_attn(loop.cache, qa, qr, loop.w_uv, mlra.SCALE_FOLDED if folded else loop.tau,
-                                        groups=groups, out_dtype=torch.float32)
-        assert max_rel_err(out.double().cpu().numpy(), loop.reference()) <= (1e-2 if dtype == "bf16" else 1e-5)
+                                        groups=groups)
+        assert max_rel_err(out.double().cpu().numpy(), loop.reference()) <= (1e-2 + 2.0 ** -8 if dtype == "bf16" else 1e-5)
     # the prompts come back as what they stand for
     n = max(len(r) for r in loop.rows)
     c, k = (torch.zeros((3, n, w), dtype=loop.cache.rope.dtype, device="cuda") for w in (512, 64))
@@ -96,7 +96,7 @@ def test_captured_steps(dtype, q_len):
     mk = lambda *shape: torch.randn(shape, device="cuda").to(dt)
     c_new, k_new, qn, qr = mk(3, q_len, 512), mk(3, q_len, 64), mk(3 * q_len, 128, 128), mk(3, q_len, 128, 64)
     qa = torch.empty((3 * q_len, 4, 128, 128), dtype=dt, device="cuda")
-    pos, out = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.empty((3, q_len, 128, 128), dtype=torch.float32, device="cuda")
+    pos, out = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.empty((3, q_len, 128, 128), dtype=dt, device="cuda")
     c_out, k_out = torch.zeros((3, 256, 512), dtype=dt, device="cuda"), torch.zeros((3, 256, 64), dtype=dt, device="cuda")
     zero = torch.zeros(3, dtype=torch.int32, device="cuda")
     ws = torch.empty(mlra.mlra_mx4_decode_workspace_bytes(3, q_len, 128, 1, 4, 128, 64, 4), dtype=torch.uint8, device="cuda")
