@@ -306,9 +306,10 @@ MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, in
  *   out   [batch][q_len][h][d_h] of out_dtype; lse optional [batch][q_len][n_blocks][hb] fp32
  *   softmax_scale: tau > 0, or MLRA_SCALE_FOLDED for queries from mlra_absorb_q_folded / mlra2_absorb_q_folded
  * The arithmetic of a bf16 call with a bf16 output is that of a cache of type dtype that holds the same values: queries (with
- * the softmax scale), probabilities and merged values are rounded to bf16, or the queries of a group of 32 channels to 2^-10 of
- * its largest (2^-15 where that stands out).  fp32 rounds nothing to fewer than 24 bits, and neither do the fp32 outputs of a
- * bf16 call (out with out_dtype MLRA_F32, or lse): they are exact to fp32, by kernels that take about twice the time.
+ * the softmax scale), probabilities and merged values are rounded to bf16, or the queries of a group of 32 channels to 2^-8 of
+ * its largest (2^-13 where that stands out), 0.11 % in the mean.  fp32 rounds nothing to fewer than 24 bits, and neither do the fp32 outputs of a
+ * bf16 call (out with out_dtype MLRA_F32, or lse): they are exact to fp32, for an out by kernels that take about
+ * twice the time.
  * A query without a row gives zeros and lse = -inf.  d_cb <= 512,
  * d_r <= 128; preconditions on pages and lengths as for mlra_decode_attn.  Deterministic. */
 MLRA_API int mlra_mx4_decode_attn(const mlra_mx4_cache* cache, int32_t batch, int32_t q_len, int32_t h, int32_t d_h,

@@ -255,7 +255,8 @@ using mx4_tile::u32x6;
 // 16-tile launch of 16 sequences of 16K tokens.
 constexpr int kFitOverhead = 10;
 
-template <int STAGES, int MODE, bool MX4>   // MODE 0: plain, 1: PAIRED, 2: GLA (see the head of the file)
+// MODE 0: plain, 1: PAIRED, 2: GLA (see the head of the file); EXACT (MX4): a log-sum-exp exact to fp32 is wanted
+template <int STAGES, int MODE, bool MX4, bool EXACT = false>
 __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   constexpr bool PAIRED = MODE != 0;                        // two 128-channel latent tiles per stage, 64 heads
@@ -556,7 +557,9 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // the first score MFMA of a tile takes that vector as its accumulator input, so the scores come out of
   // the matrix pipe already relative to the reference and feed exp2 directly.  (GLA: the two waves whose
   // partial scores are added each start from half of it; halving is exact.)
-  float m_run[2] = {0.f, 0.f};
+  // EXACT: the same before the factor tau * log2(e), which goes on in front of exp2, and the row sums are of probabilities that
+  // are not rounded yet.
+  float m_run[2] = {0.f, 0.f}, l_sum[2] = {0.f, 0.f};
   f32x16 negm[2];
   // Row sums l = sum_t P[t][head] come from the matrix pipe as well: one 16x16x32 MFMA per P^T operand
   // with a 0/1 selector as A.  Read as a 16x16x32 B operand, lane (16 b + c) of a P^T register holds head
@@ -570,7 +573,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) row_sel[e] = v;
   }
-  const float sc = p.scale_log2;
+  const float sc = p.scale_log2, lazy = EXACT ? kLazy / sc : kLazy;
 
   typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_ptr;
   typedef const __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
@@ -708,7 +711,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // has already produced relative to the old reference, are shifted.  (Rare; call settle_acc first.)
   auto rescale = [&](auto nt_tag, float d, f32x16& next_scores) {
     constexpr int nt = decltype(nt_tag)::value;
-    const float alpha = __builtin_amdgcn_exp2f(-d);
+    const float alpha = __builtin_amdgcn_exp2f(EXACT ? -d * sc : -d);
+    if (EXACT) l_sum[nt] *= alpha;
     acc_scale<16 * (0 + nt), 16>(alpha);
     acc_scale<16 * (2 + nt), 16>(alpha);
     acc_scale<16 * (4 + nt), 16>(alpha);
@@ -728,8 +732,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // the reference maximum) and their rounding to bf16 into the PV B operand: two pieces, so that the
   // rounding can sit one MFMA after the exponentials it consumes.
   auto prob_exp = [&](const f32x16& sv, int r, float& p0, float& p1) {
-    p0 = __builtin_amdgcn_exp2f(sv[r]);
-    p1 = __builtin_amdgcn_exp2f(sv[r + 1]);
+    p0 = __builtin_amdgcn_exp2f(EXACT ? sv[r] * sc : sv[r]);
+    p1 = __builtin_amdgcn_exp2f(EXACT ? sv[r + 1] * sc : sv[r + 1]);
     asm volatile("" : "+v"(p0), "+v"(p1));   // computed here, not sunk to the first use
   };
   // Row sums and Z^T += V^T P^T on the fixed accumulation registers (see acc_pv_mfma).  A tile is read and
@@ -810,7 +814,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // The factor tau * log2(e) goes into the queries, once, so that the matrix pipe delivers scores in the
   // log2 domain: each query element is multiplied in fp32 and rounded to bf16 again (queries that arrive
   // already multiplied, scale_log2 == 1, go straight from LDS into the accumulation registers).
-  const bool q_ready = sc == 1.0f;
+  const bool q_ready = EXACT || sc == 1.0f;
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt) {
     const int row = hw * 64 + nt * 32 + c32;                       // q_abs row of this lane's head column
@@ -834,10 +838,10 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         for (int i = 0; i < 4; ++i) {
           const bf16x8 part = *(lds_bf16x8_ptr)(size_t)(q_lds + row * (kDcb * 2) + (((8 * ks + 4 * g + i) ^ (row & 15)) << 4));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[8 * i + e] = (float)part[e] * sc;
+          for (int e = 0; e < 8; ++e) v[8 * i + e] = EXACT ? (float)part[e] : (float)part[e] * sc;
         }
         u32x6 rows[3];
-        const unsigned bytes = mx4_tile::split_query(v, rows, third);
+        const unsigned bytes = mx4_tile::split_query(v, rows, third, EXACT);
         qmx_sc[nt] |= (bytes & 0xffffu) << (16 * ks);
         qmx_sc3[nt] |= (bytes >> 16) << (16 * ks);
 #pragma unroll
@@ -961,7 +965,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   // codes are widened and its RoPE rows were read in the previous step, and takes tile j + 1 + STAGES; tile STAGES goes out
   // here.)
   unsigned st_cur = 0, ring_cur = 0;
-  const bool third_any = MX4 && __any(third);
+  const bool third_any = EXACT || (MX4 && __any(third));
   if (MX4) {
     wait_vm_lgkm<63>();
     __builtin_amdgcn_s_barrier();
@@ -1011,8 +1015,12 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
           const int pi = i - 1;
           if (pi < 8) prob_pack(2 * pi, pr[2 * (pi & 1)], pr[2 * (pi & 1) + 1], pb0);
           else prob_pack(2 * (pi - 8), pr[2 * (pi & 1)], pr[2 * (pi & 1) + 1], pb1);
+          if (EXACT) l_sum[pi >> 3] += pr[2 * (pi & 1)] + pr[2 * (pi & 1) + 1];
         }
-        if (i == 15) prob_pack(14, pr[2], pr[3], pb1);
+        if (i == 15) {
+          prob_pack(14, pr[2], pr[3], pb1);
+          if (EXACT) l_sum[1] += pr[2] + pr[3];
+        }
         if (i >= 6 && i < 14) load_v_part(lat_cur, (i - 6) >> 2, (i - 6) & 3, va);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -1064,7 +1072,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       const int ss = m >> 3, mt = (m >> 1) & 3;
       if ((m & 1) == 0) pv_mfma(mt, 0, va[ss][mt], pb0[ss]);
       else pv_mfma(mt, 1, va[ss][mt], pb1[ss]);
-      if (m == 0 || m == 8) {
+      if (!EXACT && (m == 0 || m == 8)) {
         row_sum_mfma(0, pb0[ss]);
         row_sum_mfma(1, pb1[ss]);
       }
@@ -1148,14 +1156,14 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         // end of the step so that the branch there finds its condition ready)
         float mx_both;
         asm("v_max_f32 %0, %1, %2" : "=v"(mx_both) : "v"(mx0), "v"(mx1));
-        need_any = __any(mx_both > kLazy);
+        need_any = __any(mx_both > lazy);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     // the maxima are relative to the reference: it moves only when a head's scores outgrow it by 2^kLazy
     // (an issuing step always has a next tile)
     if (__builtin_expect((ISSUE || has_next) && need_any, 0)) {
-      const bool need0 = mx0 > kLazy, need1 = mx1 > kLazy;
+      const bool need0 = mx0 > lazy, need1 = mx1 > lazy;
       settle_acc();
       rescale(std::integral_constant<int, 0>{}, need0 ? mx0 : 0.f, n0);
       rescale(std::integral_constant<int, 1>{}, need1 ? mx1 : 0.f, n1);
@@ -1211,6 +1219,13 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   float l_run[2];
   l_run[0] = acc_read<128>();   // (already summed over both token halves of the wave)
   l_run[1] = acc_read<132>();
+  if (EXACT) {
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      l_run[nt] = l_sum[nt] + __shfl_xor(l_sum[nt], 32);
+      m_run[nt] *= sc;
+    }
+  }
   __builtin_amdgcn_s_barrier();     // every wave is past its last tile read: the stages can be reused
   asm volatile("" ::: "memory");
   float* mbuf = (float*)smem;                 // [4 waves][64 heads]
@@ -1420,7 +1435,7 @@ int launch_decode_gla(const DecodeArgs& a) {
   return check_launch();
 }
 
-template <int STAGES, int MODE, bool MX4>
+template <int STAGES, int MODE, bool MX4, bool EXACT = false>
 static int launch_form(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) {
   constexpr int blocks = MODE == 1 ? 2 : 1;
   constexpr int lds = MX4 ? mx4_ring_bytes(blocks) + STAGES * (4 * (blocks * 1024 + 256) + kRopeBytes)
@@ -1429,12 +1444,12 @@ static int launch_form(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) 
   static PerDeviceSetup setup;
   int dev = -1;
   if (setup.needed(&dev)) {
-    if (hipFuncSetAttribute((const void*)decode_mfma_kernel<STAGES, MODE, MX4>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                            lds) != hipSuccess)
+    if (hipFuncSetAttribute((const void*)decode_mfma_kernel<STAGES, MODE, MX4, EXACT>,
+                            hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
       return MLRA_ERR_LAUNCH;
     setup.done(dev);
   }
-  MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<STAGES, MODE, MX4>), dim3(n_wg), dim3(256), lds, a.stream, p);
+  MLRA_LAUNCH_TIMED(a.t_main, (decode_mfma_kernel<STAGES, MODE, MX4, EXACT>), dim3(n_wg), dim3(256), lds, a.stream, p);
   return check_launch();
 }
 
@@ -1476,6 +1491,9 @@ int launch_decode_mfma(const DecodeArgs& a) {
     p.chunk_out = a.chunk_tab;
   }
   if (want_seq_order(a, n_wg) && launch_seq_order(a) == MLRA_OK) p.seq_order = a.seq_order;
+  if (a.precise)
+    return paired ? launch_form<kStagesPairedMx4, 1, true, true>(a, p, (unsigned)n_wg)
+                  : launch_form<kStagesMx4, 0, true, true>(a, p, (unsigned)n_wg);
   if (a.scales)
     return paired ? launch_form<kStagesPairedMx4, 1, true>(a, p, (unsigned)n_wg) : launch_form<kStagesMx4, 0, true>(a, p, (unsigned)n_wg);
   return paired ? launch_form<kStagesPaired, 1, false>(a, p, (unsigned)n_wg) : launch_form<kStages, 0, false>(a, p, (unsigned)n_wg);

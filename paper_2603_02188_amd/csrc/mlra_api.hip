@@ -154,9 +154,12 @@ struct Route {
 // A cache in 4 bits on the pipelined kernels, where they take its shape: blocks of 128 channels, or one of 512.  Up to 32 heads
 // on a block without a neighbour leave three quarters of a workgroup idle, and the kernel for every shape is ahead (one block,
 // 32 heads, whole steps: 100 sequences of 8000 tokens 64 us against 87, 4 of 8192 26 against 30; 48 heads 80 and 88, 30 and 30,
-// 16 of 16K 44 and 42).
+// 16 of 16K 44 and 42).  They move scales and queries in pieces of 16 bytes; scales, queries and weights that do not start at a
+// multiple of that take the kernel and the epilogue that read them as they lie.
 static bool mx4_pipelined(const DecodeArgs& a) {
-  return !a.precise && ((decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a));
+  const bool aligned = ((uintptr_t)a.scales | (uintptr_t)a.q_abs | (uintptr_t)a.q_rope | (uintptr_t)a.w_uv) % 16 == 0;
+  const bool exact_lse = a.precise && a.out_dtype == MLRA_BF16;       // the kernel for blocks of 128 channels has a form for it
+  return aligned && (!a.precise || (exact_lse && a.d_cb == 128)) && ((decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a));
 }
 
 // Which kernels a call takes, from its shape; sets a.fitted and a.fit_tiles.
@@ -173,7 +176,8 @@ static Route choose_route(DecodeArgs& a) {
              : decode_gla_supported(a) ? kGla
              : decode_f32_supported(a) ? kF32
                                        : kPlain;
-  r.merge_mfma = merge_upproj_mfma_supported(a) && !(a.precise && a.out_dtype == MLRA_F32);
+  r.merge_mfma = merge_upproj_mfma_supported(a) && !(a.precise && a.out_dtype == MLRA_F32) &&
+                 !(a.scales && (uintptr_t)a.w_uv % 16 != 0);
   a.fitted = r.kernel == kMlra ? r.merge_mfma && a.batch / a.q_group <= 64 &&
                                      (a.q_group > 1 || (a.plan.target_chunks > 0 && !a.plan.single_if_uniform))
              : r.kernel == kMla ? mla_mfma_fits_chunks(a)

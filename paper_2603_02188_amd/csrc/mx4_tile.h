@@ -45,11 +45,13 @@ __device__ __forceinline__ u32x4 decode8(unsigned codes, float scale) {
 }
 
 // 32 query channels, one group of the cache's side, as the sum of rows of E2M3 numbers (four significant bits, up to 7.5) with a
-// power of two each, 2^-5 apart, for v_mfma_scale_f32_*_f8f6f4.  Two rows leave 2^-10 of the largest channel at most, on normal
-// channels less than bf16 leaves of a query in the mean (0.11 % against 0.165 %).  That is no longer so where a channel is far
-// above the rest, which the two rows round as coarsely as it: if the largest is more than eight times the mean magnitude, a
-// third row is wanted, after which 2^-15 of it is left.  The first row takes the next power of two from 1.875 2^e on; a group
-// with an infinity or a NaN is NaN.  Returns the scale bytes, hi | lo << 8 | third << 16.
+// power of two each for v_mfma_scale_f32_*_f8f6f4.  Two rows 2^-5 apart leave 2^-9 of the largest channel, 2^-8 where the second
+// one is cut off (it holds 7.5 of the 8 units that the first can leave), and on normal channels less than bf16 leaves of a query
+// in the mean (0.11 % against 0.165 %).  That is no longer so where a channel is far above the rest, which the two rows round as
+// coarsely as it: if the largest is more than eight times the mean magnitude, three rows are wanted, of units 1, 2^-4 and 2^-9,
+// none of which cuts off: 2^-13 of the largest is left, and nothing of a bf16 number down to 2^-6 of it.  all: every group wants
+// them.  The first row takes the next power of two from 1.875 2^e on; a group with an infinity or a NaN is NaN.  Returns the
+// scale bytes, first | second << 8 | third << 16.
 typedef __attribute__((ext_vector_type(6))) unsigned u32x6;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
@@ -60,17 +62,19 @@ __device__ __forceinline__ u32x6 query_row(const f32x32& v, float scale) {
   for (int e = 0; e < 32; ++e) x[e] = (__bf16)v[e];
   return __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, scale);
 }
-__device__ __forceinline__ unsigned split_query(f32x32 v, u32x6 (&rows)[3], bool& third) {
+__device__ __forceinline__ unsigned split_query(f32x32 v, u32x6 (&rows)[3], bool& third,
+                                                bool all = false) {
   float top = 0.f, sum = 0.f;
 #pragma unroll
   for (int e = 0; e < 32; ++e) {
     top = fmaxf(top, fabsf(v[e]));
     sum += fabsf(v[e]);
   }
-  const bool wanted = 4.f * top > sum, finite = sum < INFINITY;   // (a NaN is in the sum)
+  const bool wanted = all || 4.f * top > sum, finite = sum < INFINITY;   // (a NaN is in the sum)
   third |= wanted;
   const int ex = min(max((int)((__float_as_uint(top) + 0x100000u) >> 23) - 2, 12), 252);
-  auto scale = [&](int t) { return __uint_as_float((unsigned)(ex - 5 * t) << 23); };
+  const int ex1 = wanted ? ex - 4 : ex - 5, ex2 = ex - 9;
+  auto scale = [&](int t) { return __uint_as_float((unsigned)(t == 0 ? ex : t == 1 ? ex1 : ex2) << 23); };
   rows[0] = query_row(v, scale(0));
   v -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(rows[0], scale(0));
   rows[1] = query_row(v, scale(1));
@@ -79,7 +83,7 @@ __device__ __forceinline__ unsigned split_query(f32x32 v, u32x6 (&rows)[3], bool
     v -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(rows[1], scale(1));
     rows[2] = query_row(v, scale(2));
   }
-  return finite ? (unsigned)ex | (unsigned)(ex - 5) << 8 | (unsigned)(ex - 10) << 16 : 0xffffffu;
+  return finite ? (unsigned)ex | (unsigned)ex1 << 8 | (unsigned)ex2 << 16 : 0xffffffu;
 }
 
 // Operands of the builtin, whose registers behind the format's are not read
