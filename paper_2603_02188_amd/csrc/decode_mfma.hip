@@ -38,7 +38,11 @@
 // latent channels cost half of what they do in bf16.  The RoPE channels stay bf16.  For the values, whose scales run along the
 // wrong axis for that instruction (a scale per token, which is the k index there), two tiles are widened to bf16, which is
 // exact: each wave widens the 16 rows that it loaded itself, tile j + 2 behind the value MFMAs of step j, into the place of
-// tile j.
+// tile j.  64 sequences of 8192 tokens, 128 heads, four blocks: 137 us, 1.25 PFLOP/s of the model's operations (172 us with the
+// scores in bf16); the matrix pipe is busy for 56 % of it.
+// EXACT, for a log-sum-exp beside a bf16 output: queries as they are, in three rows, the softmax scale in front of exp2 and row
+// sums on the vector pipe, of probabilities that are not rounded.  128 sequences of 512 to 8192 tokens, whole steps: 187 us, 172
+// without the log-sum-exp, 436 on the kernel for every shape.
 #include "chunk_fit.h"
 #include "mfma_tile.h"
 #include "mx4_tile.h"

@@ -16,6 +16,9 @@
 //     and the merge, on the fp32 matrix instructions, differ from a bf16 output's.
 //   * the running maximum moves only when a tile outgrows it by more than 2^8; (m, l, Z) is consistent for any reference.
 //   * rows are 16 bytes longer than their channels, so that sixteen rows start in sixteen different bank groups.
+// Bound by the vector instructions of a tile (widening, splitting, softmax: 600 to 700 a wave) and their latency.  fp32, 8
+// sequences of 300 to 2048 tokens, 128 heads, four blocks: 32 us, and 17 for the merge; bf16 with an fp32 output, 16 sequences of
+// 1000 to 4093, four query tokens: 155 us, and 51 for the merge.
 #include "f32_tile.h"
 #include "mx4_tile.h"
 
