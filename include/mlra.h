@@ -310,7 +310,7 @@ MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, in
  * its largest (2^-13 where that stands out), 0.11 % in the mean.  fp32 rounds nothing to fewer than 24 bits, and neither do an
  * fp32 out of a bf16 call (out_dtype MLRA_F32) and the lse beside it, by a kernel that takes about twice the time.  Beside a bf16
  * out, lse is exact to fp32 but for query channels below 2^-6 of their group's largest, which are rounded to 2^-15 of that (blocks
- * of 128 channels; others take the slower kernel).
+ * of 128 channels and MLA; others take the slower kernel).
  * A query without a row gives zeros and lse = -inf.  Scales, queries and weights may start at any multiple of their element's
  * size; at multiples of 16 bytes the faster kernels take them.  d_cb <= 512, d_r <= 128; preconditions on pages and lengths as
  * for mlra_decode_attn.  Deterministic. */

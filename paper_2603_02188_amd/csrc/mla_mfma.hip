@@ -439,7 +439,10 @@ constexpr int kXThird = kPLds + kXShift;       // third rows of the queries, 12 
 constexpr int kXThirdBytes = 8 * 64 * 24, kXLds = kXThird + 2 * kXThirdBytes;
 static_assert(kXLds <= 160 * 1024, "one workgroup per CU");
 
-template <bool MX4>
+// EXACT (4 bits, a log-sum-exp exact to fp32 is wanted): all queries as three numbers.  (The softmax scale is behind the scores
+// and the row sums are of unrounded probabilities in any case.)  64 sequences of 512 to 4096 tokens, whole steps: 119 us, 103
+// without the log-sum-exp, 313 on the kernel for every shape.
+template <bool MX4, bool EXACT = false>
 __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   constexpr int kStageB = MX4 ? kXStage : kMStage, kRopeOff = MX4 ? kXRope : kMLatBytes;
   constexpr int kPP = kPPOff + (MX4 ? kXShift : 0), kPA = kPAOff + (MX4 ? kXShift : 0), kPX = kPXOff + (MX4 ? kXShift : 0),
@@ -564,7 +567,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
           for (int e = 0; e < 8; ++e) v[8 * e8 + e] = (float)part[e];
         }
         mx4_tile::u32x6 rows[3];
-        qmx_sc[i][ks] = mx4_tile::split_query(v, rows, third);
+        qmx_sc[i][ks] = mx4_tile::split_query(v, rows, third, EXACT);
         qmx[i][ks][0] = rows[0];
         qmx[i][ks][1] = rows[1];
         if (th == 0) {               // (both waves of these heads have the same)
@@ -677,7 +680,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     typedef __attribute__((address_space(3))) mx4_tile::u32x4* u32x4_ptr;
     *(u32x4_ptr)(size_t)((lat + wd_out[r]) ^ (i << 4)) = mx4_tile::decode8(wd_raw[r][i], mx4_tile::scale_of(wd_byte[r]));
   };
-  const bool third_any = MX4 && __any(third);
+  const bool third_any = EXACT || (MX4 && __any(third));
   // scores of a tile whose operands are read, with the operands of the value product of the tile before it and (with_v) the tile
   // itself widened into wl
   auto scores_mx4 = [&](unsigned vb, int par, auto with_v, unsigned wl) {
@@ -996,17 +999,17 @@ static int launch_mla_as(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg
   return check_launch();
 }
 
-template <bool MX4>
+template <bool MX4, bool EXACT = false>
 static int launch_mla_pipe(const DecodeArgs& a, const MfmaParams& p, unsigned n_wg) {
   constexpr int lds = MX4 ? kXLds : kPLds;
   static PerDeviceSetup setup;
   int setup_dev = -1;
   if (setup.needed(&setup_dev)) {
-    if (hipFuncSetAttribute((const void*)mla_pipe_kernel<MX4>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    if (hipFuncSetAttribute((const void*)mla_pipe_kernel<MX4, EXACT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
       return MLRA_ERR_LAUNCH;
     setup.done(setup_dev);
   }
-  MLRA_LAUNCH_TIMED(a.t_main, mla_pipe_kernel<MX4>, dim3(n_wg), dim3(256), lds, a.stream, p);
+  MLRA_LAUNCH_TIMED(a.t_main, (mla_pipe_kernel<MX4, EXACT>), dim3(n_wg), dim3(256), lds, a.stream, p);
   return check_launch();
 }
 
@@ -1060,6 +1063,7 @@ int launch_mla_mfma(const DecodeArgs& a) {
   if (!a.balanced && !a.fitted && (n_wg > a.cus || a.q_group > 1) && launch_seq_order(a) == MLRA_OK) p.seq_order = a.seq_order;
   // (the query tokens of one sequence are kept side by side in the order)
   p.split_major = p.seq_order && a.q_group <= 1;
+  if (a.precise) return launch_mla_pipe<true, true>(a, p, (unsigned)n_wg);
   if (a.scales) return launch_mla_pipe<true>(a, p, (unsigned)n_wg);
   const int stages = mla_mfma_stages(a);
   if (stages == 4) return launch_mla_as<4>(a, p, (unsigned)n_wg);

@@ -158,8 +158,7 @@ struct Route {
 // multiple of that take the kernel and the epilogue that read them as they lie.
 static bool mx4_pipelined(const DecodeArgs& a) {
   const bool aligned = ((uintptr_t)a.scales | (uintptr_t)a.q_abs | (uintptr_t)a.q_rope | (uintptr_t)a.w_uv) % 16 == 0;
-  const bool exact_lse = a.precise && a.out_dtype == MLRA_BF16;       // the kernel for blocks of 128 channels has a form for it
-  return aligned && (!a.precise || (exact_lse && a.d_cb == 128)) && ((decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a));
+  return aligned && (!a.precise || a.out_dtype == MLRA_BF16) && ((decode_mfma_supported(a) && (a.h > 32 || decode_mfma_paired(a.h, a.n_blocks, a.groups))) || mla_mfma_supported(a));
 }
 
 // Which kernels a call takes, from its shape; sets a.fitted and a.fit_tiles.

@@ -25,7 +25,7 @@ def _check(lens, out=None, **kw):
     """bf16 calls with a bf16 output, on the bf16 kernels, without and with the log-sum-exp, and with both in fp32."""
     if out is None and kw.get("dtype", "bf16") == "bf16":
         _case(lens, out="bf16", with_lse=False, **kw)
-        if kw.get("d_cb", 128) == 128:
+        if kw.get("d_cb", 128) in (128, 512):
             _case(lens, out="bf16", **kw)
     _case(lens, out=out or "f32", **kw)
 
@@ -81,7 +81,7 @@ def _case(lens, n_blocks=4, d_cb=128, d_r=64, h=128, d_h=128, groups=1, q_len=1,
         # query beside a bf16 output (see _query_rest); a log-sum-exp moves by no more than the score that moves most.
         size = max(1.0, float(np.abs(ref_lse[~empty]).max()))
         bar = 5.0 * 2.0 ** -24 / np.sqrt(3.0) * np.sqrt(3.0 * d_cb + 6.0 * d_r) * size + 1e-6
-        rest = _query_rest(hc.rows, qa64, tau, groups) if dtype == out == "bf16" and d_cb == 128 else 0.0
+        rest = _query_rest(hc.rows, qa64, tau, groups) if dtype == out == "bf16" and d_cb in (128, 512) else 0.0
         assert (np.abs(lse[~empty] - ref_lse[~empty]) <= (bar + rest * np.ones(lse.shape))[~empty]).all()
     for s, n in enumerate(lens):
         for j in range(q_len):
