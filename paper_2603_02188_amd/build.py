@@ -15,9 +15,9 @@ import sys
 from concurrent.futures import ThreadPoolExecutor
 
 try:
-    from .check_isa import find_overlaps, find_reserved_acc_uses, find_scratch_in_loops
+    from .check_isa import find_overlaps, find_reserved_acc_uses, find_scratch_in_loops, find_unwaited_lds_writes
 except ImportError:  # run as a script
-    from check_isa import find_overlaps, find_reserved_acc_uses, find_scratch_in_loops
+    from check_isa import find_overlaps, find_reserved_acc_uses, find_scratch_in_loops, find_unwaited_lds_writes
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -29,6 +29,9 @@ HIP_FLAGS = [
     "-mllvm", "-amdgpu-mfma-vgpr-form",   # MFMA results in VGPRs: AGPRs are left to the pinned query operands
     "-Wno-unused-command-line-argument",
 ]
+
+# decode_mfma_kernel<STAGES, MODE, MX4 = true, EXACT>, mangled
+MX4_DECODE = r"decode_mfma_kernelILi\d+ELi\d+ELb1E"
 
 
 def _hipcc() -> str:
@@ -76,6 +79,11 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
         bad = find_scratch_in_loops(text, r"mla_(mfma|pipe)_kernel")
         if bad:
             raise RuntimeError(f"{src}: scratch accesses inside the loop of an MLA kernel:\n" +
+                               "\n".join(f"  {asm}:{ln}: {text}" for ln, text in bad[:20]))
+        # the decode kernel's barriers wait for nothing by themselves: its forms on a cache in 4 bits write to LDS by hand
+        bad = find_unwaited_lds_writes(text, MX4_DECODE)
+        if bad:
+            raise RuntimeError(f"{src}: barriers that an LDS write may pass:\n" +
                                "\n".join(f"  {asm}:{ln}: {text}" for ln, text in bad[:20]))
         return obj
 

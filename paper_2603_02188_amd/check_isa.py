@@ -3,8 +3,8 @@
 An MFMA with a destination wider than four registers must not write registers it still reads as srcA /
 srcB (the narrow forms, 16x16 results of four registers, read their operands before the first write and
 may overlap).  The build runs this over every kernel's assembly and fails if such an instruction was
-emitted.  Two more scans are for single kernels: accumulation registers that belong to inline asm, and spills inside a
-loop.
+emitted.  Three more scans are for single kernels: accumulation registers that belong to inline asm, spills inside a
+loop, and barriers that an LDS write has not been waited for in front of.
 """
 from __future__ import annotations
 
@@ -86,6 +86,74 @@ def find_scratch_in_loops(asm_text: str, kernel_pattern: str):
         elif in_kernel and in_loop and re.match(r"(scratch_|buffer_(load|store)_\w+ .*\boffset:.*\bs\[0:3\])", text):
             bad.append((ln, text))
     return bad
+
+
+_LABEL = re.compile(r"^([A-Za-z_.$][\w.$]*):")
+_LDS_OP = re.compile(r"^ds_(?!nop\b)(\w+)")
+_LGKM = re.compile(r"\blgkmcnt\((\d+)\)")
+
+
+def _lds_writes(op: str) -> bool:
+    """Whether ds_<op> changes LDS (reads, swizzles and permutes do not)."""
+    return not op.startswith(("read", "bpermute", "permute", "swizzle", "consume", "append", "load"))
+
+
+def find_unwaited_lds_writes(asm_text: str, kernel_pattern: str):
+    """Barriers of the kernels whose name matches kernel_pattern that a wave can reach with an LDS write of its own still under
+    way: s_barrier does not wait for one, so that it may land on top of what another wave stores behind the barrier.  LDS
+    operations of a wave end in order: s_waitcnt lgkmcnt(n) leaves the last n under way at most (scalar loads, which count as
+    well, only make it stricter).  The state is the least number of LDS operations behind the last write over all paths."""
+    bad = []
+    lines, start = asm_text.splitlines(), None
+    for ln, line in enumerate(lines + ["end:"]):
+        m = _LABEL.match(line)
+        if not m or m.group(1).startswith("."):
+            continue
+        if start is not None:
+            bad += _unwaited_in(lines, start, ln)
+        start = ln + 1 if re.search(kernel_pattern, m.group(1)) else None
+    return bad
+
+
+def _unwaited_in(lines, first, last):
+    blocks, names, cur = [[]], {}, 0             # per block: (line, instruction); which block a label starts
+    for ln in range(first, last):
+        m = _LABEL.match(lines[ln])
+        if m:
+            blocks.append([])
+            names[m.group(1)] = len(blocks) - 1
+            continue
+        text = lines[ln].split(";")[0].strip()
+        if not text or text.startswith("."):
+            continue
+        blocks[-1].append((ln, text))
+        if text.startswith(("s_branch", "s_cbranch", "s_endpgm")):
+            blocks.append([])
+    kNone = 1 << 20                              # nothing under way
+    state = [None] * len(blocks)                 # at the head of a block; None: not reached yet
+    state[0], todo, found = kNone, [0], {}
+    while todo:
+        b = todo.pop()
+        k, nexts = state[b], [b + 1]
+        for ln, text in blocks[b]:
+            op = _LDS_OP.match(text)
+            if op:
+                k = 0 if _lds_writes(op.group(1)) else k + 1 if k < 64 else k
+            elif text.startswith("s_waitcnt"):
+                n = _LGKM.search(text)
+                if n and k >= int(n.group(1)):
+                    k = kNone
+            elif text.startswith("s_barrier") and k < kNone:
+                found[ln + 1] = text
+            if text.startswith(("s_branch", "s_cbranch")):
+                nexts = [names[text.split()[1]]] + ([] if text.startswith("s_branch") else [b + 1])
+            elif text.startswith("s_endpgm"):
+                nexts = []
+        for n in nexts:
+            if n < len(blocks) and (state[n] is None or k < state[n]):
+                state[n] = k
+                todo.append(n)
+    return sorted(found.items())
 
 
 if __name__ == "__main__":

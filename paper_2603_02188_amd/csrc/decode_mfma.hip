@@ -1230,6 +1230,10 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       m_run[nt] *= sc;
     }
   }
+  if (MX4) {      // (the last step has widened a tile into the ring, which nothing reads: it lands before the ring is reused)
+    wait_vm_lgkm<63>();
+    asm volatile("" ::: "memory");
+  }
   __builtin_amdgcn_s_barrier();     // every wave is past its last tile read: the stages can be reused
   asm volatile("" ::: "memory");
   float* mbuf = (float*)smem;                 // [4 waves][64 heads]
