@@ -813,6 +813,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   for (int jj = 1; jj < STAGES - kQStages && jj < ntiles; ++jj) issue_tile();
   if (GLA && tid < 4) ((float*)(smem + STAGES * kStageB))[tid] = 0.f;   // the zeros some RoPE reads below take
   // queries landed (they are older than the tile loads; vector-memory operations retire in order) ...
+  if (GLA) wait_vm_lgkm<63>();    // (and the zeros)
   if (ntiles >= STAGES - kQStages) wait_vmcnt<kLoadsTile * (STAGES - kQStages)>(); else wait_vmcnt<0>();
   __builtin_amdgcn_s_barrier();   // ... in every wave's share
   // The factor tau * log2(e) goes into the queries, once, so that the matrix pipe delivers scores in the
