@@ -64,13 +64,15 @@ __device__ __forceinline__ u32x6 query_row(const f32x32& v, float scale) {
 }
 __device__ __forceinline__ unsigned split_query(f32x32 v, u32x6 (&rows)[3], bool& third,
                                                 bool all = false) {
-  float top = 0.f, sum = 0.f;
+  float top = 0.f, sum = 0.f;      // (of 1/64 of the magnitudes, which no 32 finite ones overflow)
 #pragma unroll
   for (int e = 0; e < 32; ++e) {
     top = fmaxf(top, fabsf(v[e]));
-    sum += fabsf(v[e]);
+    sum = fmaf(fabsf(v[e]), 1.f / 64.f, sum);
   }
-  const bool wanted = all || 4.f * top > sum, finite = sum < INFINITY;   // (a NaN is in the sum)
+  const bool finite = sum < INFINITY;        // (a NaN is in the sum)
+  // (from 0x1.ep127 on the first row is cut off, which one more cannot make good)
+  const bool wanted = all || top * (1.f / 16.f) > sum || (finite && top >= 0x1.ep127f);
   third |= wanted;
   const int ex = min(max((int)((__float_as_uint(top) + 0x100000u) >> 23) - 2, 12), 252);
   const int ex1 = wanted ? ex - 4 : ex - 5, ex2 = ex - 9;
