@@ -80,10 +80,16 @@ __device__ __forceinline__ short4v read_tr16(const __bf16* p) {
       (short4v __attribute__((address_space(3)))*)(__attribute__((address_space(3))) const __bf16*)p);
 }
 
+// Waves on a SIMD that the registers of the fp32 shapes leave room for, but for the seldom taken ways (0: as it comes)
+template <typename T, int DP, int RP, int NH>
+constexpr int min_waves() {
+  return Terms<T>::n == 1 || DP * NH > 128 || NH * RP > 128 ? 0 : DP == 64 && RP == 64 && NH == 1 ? 3 : 2;
+}
+
 // DP, RP: latent and RoPE channels of the tile, at least d_cb and d_r; VEC: RoPE rows and queries in pieces of four elements
 // PT: bf16 terms of a probability
 template <typename T, int DP, int RP, int NH, bool VEC, int PT>
-__global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
+__global__ __launch_bounds__(256, (min_waves<T, DP, RP, NH>())) void mx4_decode_kernel(Mx4Params p) {
   typedef typename RawOf<T>::type Raw;
   constexpr int N = Terms<T>::n;
   constexpr int LP = DP + 8, PP = RP + 8;                    // elements per row of the latent / RoPE tile
@@ -286,6 +292,38 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
             for (int tt = 0; tt < 2; ++tt)
               sc[m][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c][tt], qf[m][KL + ks][i], sc[m][tt], 0, 0, 0);
     }
+    if constexpr (N > 1) {
+      // The lower terms of an infinity, and of a finite number that rounds to one in bf16, are NaN, and so is a score that they
+      // are in: it is computed again from the numbers themselves.
+      float nan = 0.f;
+#pragma unroll
+      for (int m = 0; m < NH; ++m)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) nan += (sc[m][tt][0] + sc[m][tt][1]) + (sc[m][tt][2] + sc[m][tt][3]);
+      if (__builtin_expect(__any(nan != nan), 0)) {
+#pragma unroll
+        for (int m = 0; m < NH; ++m) {
+          const int head = min(head0 + 16 * m + r16, p.h - 1);
+          const T* const qa = (const T*)p.q_abs + (((size_t)s * p.n_blocks + b) * p.h + head) * d_cb;
+          const T* const qr = (const T*)p.q_rope + ((size_t)s * p.h * p.groups + (b / (p.n_blocks / p.groups)) * p.h + head) * d_r;
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (sc[m][tt][i] == sc[m][tt][i]) continue;
+              const int in = tok0 + 16 * tt + 4 * q + i, tok = t0 + min(j * kTile + in, t1 - t0 - 1);
+              const long long page = p.page_table[(size_t)s * p.max_pages + tok / p.page_size];
+              const T* const kr = (const T*)p.rope + (page * p.page_size + tok % p.page_size) * d_r;
+              float sum = 0.f;
+#pragma unroll 1
+              for (int k = 0; k < d_cb; ++k) sum = fmaf(load_f32(qa, k), (float)lat[in * LP + k], sum);
+#pragma unroll 1
+              for (int k = 0; k < d_r; ++k) sum = fmaf(load_f32(qr, k), load_f32(kr, k), sum);
+              sc[m][tt][i] = sum;
+            }
+        }
+      }
+    }
     const int valid = t1 - t0 - j * kTile - tok0;       // tokens of this wave's share that exist
     float mx[NH], lowest = INFINITY;
     bool grown = false;
@@ -332,7 +370,7 @@ __global__ __launch_bounds__(256) void mx4_decode_kernel(Mx4Params p) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) lowest = sc[m][tt][i] > -INFINITY ? fminf(lowest, sc[m][tt][i]) : lowest;
+          for (int i = 0; i < 4; ++i) lowest = fminf(lowest, sc[m][tt][i]);      // (-inf, no token, among them)
         if (__any(lowest < -126.f)) {
 #pragma unroll
           for (int tt = 0; tt < 2; ++tt)

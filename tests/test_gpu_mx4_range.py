@@ -51,3 +51,79 @@ def test_finite_queries_whose_sum_is_not(n_blocks, d_cb, h, with_lse):
         bar = 5.0 * 2.0 ** -24 / np.sqrt(3.0) * np.sqrt(3.0 * d_cb + 6.0 * 64) * size + 1e-6
         rest = _query_rest(hc.rows, qa64, tau, 1) if d_cb in (128, 512) else 0.0
         assert (np.abs(lse.double().cpu().numpy() - ref_lse) <= bar + rest).all()
+
+
+# fp32: RoPE numbers are the sum of three of bf16 there, whose products with an infinite one are NaN or infinities of either sign
+F32 = [(4, 128, 64, 128), (2, 64, 32, 40), (1, 512, 64, 20), (2, 256, 128, 16), (2, 128, 128, 8)]
+
+
+def _f32(n_blocks, d_cb, d_r, h, lens, seed):
+    hc = HostCache(lens, n_blocks, d_cb, d_r, "f32", 64, seed)
+    rng = np.random.default_rng([seed, 1])
+    return hc, queries(rng, len(lens), 1, n_blocks, h, 1, d_cb, d_r, 32, "f32")
+
+
+def _set_key(hc, s, t, channel, value):
+    hc.rope[hc.table[s, t // hc.page], t % hc.page, channel] = hc.ropes[s][t, channel] = value
+
+
+@pytest.mark.parametrize("n_blocks,d_cb,d_r,h", F32)
+def test_a_score_of_minus_infinity_has_no_weight(n_blocks, d_cb, d_r, h):
+    """Infinite keys whose products with every query are -inf: queries that are bf16 numbers (lower terms of zero), and others."""
+    lens, tau = [200, 70], 0.1
+    hc, ((qa, qa64), (_, qr64), (wv, wv64)) = _f32(n_blocks, d_cb, d_r, h, lens, 41)
+    for s, t, channel, value in ((0, 10, 3, -np.inf), (0, 130, 3, -np.inf), (1, 0, 5, np.inf), (1, 69, 3, -np.inf)):
+        _set_key(hc, s, t, channel, value)
+    qr64[..., 3], qr64[..., 5] = np.abs(qr64[..., 3]) + 0.1, -np.abs(qr64[..., 5]) - 0.1
+    qr64[..., ::2, 3], qr64[..., ::2, 5] = 1.0, -0.5
+    qr, qr64 = stored(qr64, "f32")
+    lse = torch.empty((2, 1, n_blocks, h), device="cuda")
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, tau, lse=lse).double().cpu().numpy()
+    ref, ref_lse = orc.attend(hc.rows, hc.ropes, lens, qa64, qr64, wv64, tau)
+    err = max_rel_err(got, ref)
+    print(f"       max rel err {err:.3e}", flush=True)
+    assert err <= 1e-5
+    # (scores of about 10: see the bar in test_gpu_mx4_decode.py)
+    assert np.abs(lse.double().cpu().numpy() - ref_lse).max() <= 1e-4
+
+
+@pytest.mark.parametrize("n_blocks,d_cb,d_r,h", F32)
+def test_infinite_and_nan_numbers_reach_their_heads_only(n_blocks, d_cb, d_r, h):
+    """Heads whose product with an infinite key is +inf, and those whose query holds an infinity or a NaN, become NaN; the others'
+    tokens with -inf do not count."""
+    lens, tau = [200, 70], 0.1
+    hc, ((qa, qa64), (_, qr64), (wv, wv64)) = _f32(n_blocks, d_cb, d_r, h, lens, 42)
+    _set_key(hc, 0, 77, 2, np.inf)
+    qr64[..., 2] = np.abs(qr64[..., 2]) + 0.1
+    qr64[..., :h - 3, 2] *= -1.0                     # the last three heads see +inf in sequence 0
+    qr64[1, 0, 1, 4], qr64[1, 0, 2, 4] = np.inf, np.nan
+    qa64[1, 0, 0, 3, 9] = -np.inf
+    (qr, qr64), (qa, qa64) = stored(qr64, "f32"), stored(qa64, "f32")
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, tau).double().cpu().numpy()
+    bad = np.zeros((2, h), dtype=bool)
+    bad[0, h - 3:], bad[1, 1:4] = True, True
+    assert np.isnan(got[:, 0][bad]).all()
+    with np.errstate(invalid="ignore"):
+        ref, _ = orc.attend(hc.rows, hc.ropes, lens, qa64, qr64, wv64, tau)
+    assert np.isnan(ref[:, 0][bad]).all()
+    assert max_rel_err(got[:, 0][~bad], ref[:, 0][~bad]) <= 1e-5
+
+
+@pytest.mark.parametrize("n_blocks,d_cb,d_r,h", F32)
+def test_the_largest_finite_numbers(n_blocks, d_cb, d_r, h):
+    """Keys that round to an infinity in bf16, against queries of 1e-38."""
+    lens, tau = [200, 70], 0.1
+    hc, ((qa, qa64), (_, qr64), (wv, wv64)) = _f32(n_blocks, d_cb, d_r, h, lens, 43)
+    rng = np.random.default_rng(44)
+    for s, n in enumerate(lens):
+        for t in range(n):
+            _set_key(hc, s, t, 6, float(np.float32(rng.choice([-1.0, 1.0]) * rng.uniform(3.397e38, 3.4028e38))))
+    # (bf16 numbers: lower terms of numbers this small would be denormal)
+    qr64[..., 6] = stored(rng.uniform(1.2e-38, 6e-38, qr64[..., 6].shape), "bf16")[1]
+    qr, qr64 = stored(qr64, "f32")
+    hc.rope[np.isnan(hc.rope)] = 0.0                 # (spare slots: not to be converted with a warning)
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, tau).double().cpu().numpy()
+    ref, _ = orc.attend(hc.rows, hc.ropes, lens, qa64, qr64, wv64, tau)
+    err = max_rel_err(got, ref)
+    print(f"       max rel err {err:.3e}", flush=True)
+    assert err <= 1e-5
