@@ -120,6 +120,9 @@ MLRA_API size_t mlra_decode_workspace_bytes(int32_t batch, int32_t h, int32_t n_
  *              max_pages_per_seq*page_size) bytes, 256-byte aligned; contents are overwritten.
  *   softmax_scale: tau > 0, or MLRA_SCALE_FOLDED when q_abs and q_rope come from mlra_absorb_q_folded
  *              (they then carry tau log2(e) and the scores are not scaled again).
+ * A NaN or an infinity in a query or a row reaches its own sequence only, and in a query its own head, but for bf16 caches with
+ * blocks of 128 or 256 channels and d_r = 64: there the row sums of heads i and i + 16 (i / 16 even) come from one matrix
+ * product, and a NaN of one makes NaN of both.
  * Context is split into chunks processed by independent workgroups whose partial (max, sum, z) are
  * merged with a log-sum-exp merge; results are deterministic (no atomics). */
 MLRA_API int mlra_decode_attn(const mlra_cache* cache, int32_t batch, int32_t h, int32_t d_h, const void* q_abs,
@@ -311,7 +314,9 @@ MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, in
  * fp32 out of a bf16 call (out_dtype MLRA_F32) and the lse beside it, by a kernel that takes about twice the time.  Beside a bf16
  * out, lse is exact to fp32 but for query channels below 2^-6 of their group's largest, which are rounded to 2^-15 of that (blocks
  * of 128 channels and MLA; others take the slower kernel).
- * A query without a row gives zeros and lse = -inf.  Scales, queries and weights may start at any multiple of their element's
+ * A query without a row gives zeros and lse = -inf.  A NaN or an infinity in a query makes NaN of its own head's output (by the
+ * formula it does).  A score that overflows fp32 although query and row are finite, or that an infinite RoPE key makes infinite, can
+ * make NaN of the head 16 away as well beside a bf16 out without lse (see mlra_decode_attn).  Scales, queries and weights may start at any multiple of their element's
  * size; at multiples of 16 bytes the faster kernels take them.  d_cb <= 512, d_r <= 128; preconditions on pages and lengths as
  * for mlra_decode_attn.  Deterministic. */
 MLRA_API int mlra_mx4_decode_attn(const mlra_mx4_cache* cache, int32_t batch, int32_t q_len, int32_t h, int32_t d_h,

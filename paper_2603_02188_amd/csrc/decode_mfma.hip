@@ -809,6 +809,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   unsigned qmx_sc[2] = {0, 0};  // ... and their scales, byte 2 ks + term, of the third term byte 2 ks
   unsigned qmx_sc3[2] = {0, 0};
   bool third = false;           // a group of these queries wants its third term
+  unsigned nan_heads[2] = {0, 0};   // (MX4) heads of a tile whose query is not finite, bit c32
   issue_last_tile();
   for (int jj = 1; jj < STAGES - kQStages && jj < ntiles; ++jj) issue_tile();
   if (GLA && tid < 4) ((float*)(smem + STAGES * kStageB))[tid] = 0.f;   // the zeros some RoPE reads below take
@@ -834,6 +835,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       // the RoPE term is counted once; the other wave's channels are read from 16 bytes of zeros
       qaddr[8 + ks] = (!GLA || (ks >> 1) == hw) ? addr : lds_base + STAGES * kStageB;
     }
+    bool not_finite = false;
     if (MX4) {
       // a lane's 32 channels of operand ks, 64 ks + 32 g .. + 31, are one group
 #pragma unroll
@@ -847,6 +849,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
         }
         u32x6 rows[3];
         const unsigned bytes = mx4_tile::split_query(v, rows, third, EXACT);
+        not_finite |= bytes == mx4_tile::kNotFinite;
         qmx_sc[nt] |= (bytes & 0xffffu) << (16 * ks);
         qmx_sc3[nt] |= (bytes >> 16) << (16 * ks);
 #pragma unroll
@@ -865,6 +868,30 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       for (int ks = kFirst; ks < 12; ++ks)
 #pragma unroll
         for (int e = 0; e < 8; ++e) raw[ks][e] = (__bf16)((float)raw[ks][e] * sc);
+    }
+    if (MX4 && !EXACT) {
+      // A query with an infinity or a NaN gives NaN whatever the rows are, and nothing but its own head: the row sums' matrix
+      // product takes two heads together, so that it goes through the loop as zeros and gets its NaN behind it.
+      typedef __attribute__((ext_vector_type(8))) unsigned short ushort8;
+      typedef __attribute__((ext_vector_type(4))) unsigned short ushort4;
+      typedef __attribute__((ext_vector_type(2))) unsigned short ushort2v;
+      ushort8 t8 = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+      for (int ks = kFirst; ks < 12; ++ks)
+        t8 = __builtin_elementwise_max(t8, __builtin_bit_cast(ushort8, raw[ks]) & (unsigned short)0x7fff);
+      const ushort4 t4 = __builtin_elementwise_max(t8.lo, t8.hi);
+      const ushort2v t2 = __builtin_elementwise_max(t4.lo, t4.hi);
+      not_finite |= ((__builtin_bit_cast(unsigned, t2) + 0x00800080u) & 0x80008000u) != 0u;    // (exponent 255 in either half)
+      const unsigned long long lanes = __ballot(not_finite);
+      nan_heads[nt] = (unsigned)lanes | (unsigned)(lanes >> 32);
+      if (__builtin_expect(nan_heads[nt] != 0u, 0)) {
+        const bool mine = nan_heads[nt] >> c32 & 1;
+        if (mine) qmx_sc[nt] = qmx_sc3[nt] = 0;
+#pragma unroll
+        for (int ks = kFirst; ks < 12; ++ks)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) raw[ks][e] = mine ? (__bf16)0.f : raw[ks][e];
+      }
     }
 #pragma unroll
     for (int ks = kFirst; ks < 12; ++ks) {
@@ -1279,6 +1306,7 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     w_par[nt] = __builtin_amdgcn_exp2f(mp - ms);
     m_out[nt] = ms;
     l_out[nt] = l_run[nt] * w_own[nt] + lp * w_par[nt];
+    if (MX4 && !EXACT && (nan_heads[nt] >> c32 & 1)) w_own[nt] = NAN;
   }
   const size_t unit = ((size_t)seq * p.n_blocks + blk) * p.n_splits + split;
   constexpr int kZRow = GLA ? 2 * kDcb : kDcb;   // channels of one partial row in the workspace (GLA: hw is the channel half)

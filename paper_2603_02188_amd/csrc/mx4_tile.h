@@ -56,6 +56,7 @@ typedef __attribute__((ext_vector_type(6))) unsigned u32x6;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
 typedef __attribute__((ext_vector_type(32))) float f32x32;
+constexpr unsigned kNotFinite = 0xffffff;     // ... NaN each
 __device__ __forceinline__ u32x6 query_row(const f32x32& v, float scale) {
   bf16x32 x;
 #pragma unroll
@@ -85,7 +86,7 @@ __device__ __forceinline__ unsigned split_query(f32x32 v, u32x6 (&rows)[3], bool
     v -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(rows[1], scale(1));
     rows[2] = query_row(v, scale(2));
   }
-  return finite ? (unsigned)ex | (unsigned)ex1 << 8 | (unsigned)ex2 << 16 : 0xffffffu;
+  return finite ? (unsigned)ex | (unsigned)ex1 << 8 | (unsigned)ex2 << 16 : kNotFinite;
 }
 
 // Operands of the builtin, whose registers behind the format's are not read

@@ -53,6 +53,38 @@ def test_finite_queries_whose_sum_is_not(n_blocks, d_cb, h, with_lse):
         assert (np.abs(lse.double().cpu().numpy() - ref_lse) <= bar + rest).all()
 
 
+@pytest.mark.parametrize("with_lse", [False, True])
+@pytest.mark.parametrize("n_blocks,d_cb,h,groups", [(4, 128, 128, 1), (4, 128, 64, 1), (2, 128, 40, 1), (4, 128, 128, 2), (3, 128, 100, 1),
+                                                    (1, 512, 64, 1), (2, 64, 16, 1)])
+def test_queries_that_are_not_finite_reach_their_heads_only(n_blocks, d_cb, h, groups, with_lse):
+    """NaN and infinities in a query's latent or RoPE channels, of one block or all: every other head, and so every other sequence,
+    is as without them to the last bit.  One chunk a sequence, and several."""
+    hb = h // groups
+    for lens in ([200, 130, 64], [2000, 130]):
+        hc = HostCache(lens, n_blocks, d_cb, 64, "bf16", 64, 51)
+        rng = np.random.default_rng(52)
+        batch = len(lens)
+        (qa, _), (qr, _), (wv, _) = queries(rng, batch, 1, n_blocks, hb, groups, d_cb, 64, 64, "bf16")
+        lse = [torch.zeros((batch, 1, n_blocks, hb), device="cuda") for _ in range(2)]
+        call = lambda a, r, l: mlra.mlra_mx4_decode_attn(hc.device(), a, r, wv, 0.07, groups=groups, lse=l if with_lse else None)
+        want = call(qa, qr, lse[0])
+        bad_a, bad_r, bad = qa.clone(), qr.clone(), torch.zeros((batch, h), dtype=torch.bool)
+        for s, b, i, c, v in ((0, 0, 5, 40, "nan"), (1, n_blocks - 1, 7, 1, "inf"), (1, 0, hb - 1, d_cb - 1, "-inf")):
+            bad_a[s, 0, b, i, c] = float(v)
+            bad[s, b // (n_blocks // groups) * hb + i] = True
+        for s, i, c, v in ((0, 3, 63, "-inf"), (0, h - 2, 0, "nan"), (1, 11, 31, "inf")):
+            bad_r[s, 0, i, c] = float(v)
+            bad[s, i] = True
+        got = call(bad_a, bad_r, lse[1])
+        assert got[:, 0][bad].isnan().all()
+        assert torch.equal(got[:, 0][~bad], want[:, 0][~bad])
+        if with_lse:                                 # (of a block; an infinite score makes an infinity or a NaN of it)
+            same = ~(bad_a.isnan() | bad_a.isinf()).any(-1)[:, 0]                           # [batch][blocks][hb]
+            rope = ~(bad_r.isnan() | bad_r.isinf()).any(-1)[:, 0].view(batch, groups, 1, hb)
+            same = (same.view(batch, groups, -1, hb) & rope).view(batch, n_blocks, hb)
+            assert torch.equal(lse[1][:, 0][same], lse[0][:, 0][same]) and not lse[1][:, 0][~same].isfinite().any()
+
+
 # fp32: RoPE numbers are the sum of three of bf16 there, whose products with an infinite one are NaN or infinities of either sign
 F32 = [(4, 128, 64, 128), (2, 64, 32, 40), (1, 512, 64, 20), (2, 256, 128, 16), (2, 128, 128, 8)]
 
