@@ -324,8 +324,7 @@ static SplitPlan plan_mx4_fast(int units, int q_len, int h, int groups, int n_bl
   if (n_seqs < 4 || n_seqs > 64 || one.chunk_tokens < (mla ? 1024 : 4096) || fills || (mla && q_len > 1)) return one;
   SplitPlan two = plan_splits(units, per_unit, max_seq_len, 2 * cus);
   // (no more slots than the bf16 epilogue takes)
-  const int bpg = n_blocks / groups, most = std::min(128 / bpg, (98176 - 64 * (bpg * d_cb + 8)) / (256 * bpg));
-  if (two.n_splits > most || two.n_splits <= one.n_splits) return one;
+  if (two.n_splits > merge_upproj_mfma_slots(n_blocks / groups, d_cb) || two.n_splits <= one.n_splits) return one;
   two.target_chunks = mla ? 0 : units;       // (fitted, see choose_route)
   return two;
 }

@@ -159,6 +159,7 @@ bool absorb_q_mfma_supported(int d_h, int d_cb, int dtype);
 int launch_absorb_q_mfma(int batch, int h, int d_h, int n_blocks, int groups, int d_cb, const void* q_nope,
                          const void* w_uk, void* q_abs, hipStream_t stream, float fold = 1.f,
                          const void* q_rope = nullptr, void* q_rope_out = nullptr, int d_r = 0);   // d_r % 8 == 0
+int merge_upproj_mfma_slots(int bpg, int d_cb);   // chunk slots of a block that it takes at most, bpg blocks per head
 bool merge_upproj_mfma_supported(const DecodeArgs& a);
 int launch_merge_upproj_mfma(const DecodeArgs& a);
 

@@ -7,6 +7,8 @@
 // per workgroup, and both put the head index on the grid.
 #include "mlra_internal.h"
 
+#include <algorithm>
+
 namespace mlra {
 namespace {
 
@@ -506,10 +508,13 @@ constexpr size_t kMergeLdsLimit = 160 * 1024;
 // channel and 256 per slot; everything else takes the fp32 epilogue (and fp32 partials).  This is no limit of the kernel:
 // with 128 bytes per slot and 32 KiB of weights it occupies up to 112 KiB of LDS here, and 256 slots at 512 channels (one
 // sequence of 8K tokens and up, four blocks) would fit; whether it is the better epilogue there has not been measured.
+int merge_upproj_mfma_slots(int bpg, int d_cb) {
+  return (int)std::min(128L / bpg, (98176 - 64L * ((long)bpg * d_cb + 8)) / (256L * bpg));
+}
 bool merge_upproj_mfma_supported(const DecodeArgs& a) {
   const int bpg = a.n_blocks / a.groups;
   return a.dtype == MLRA_BF16 && a.d_h == kDh && a.d_cb % 32 == 0 && bpg * a.d_cb <= 1024 &&
-         bpg * a.plan.n_splits <= 128 && 64L * (bpg * a.d_cb + 8) + 256L * bpg * a.plan.n_splits <= 98176;
+         a.plan.n_splits <= merge_upproj_mfma_slots(bpg, a.d_cb);
 }
 
 template <typename TO, int MODE, int U, int KK>
