@@ -387,6 +387,18 @@ MLRA_API int mlra_decode_route_info(int32_t batch, int32_t q_len, int32_t h, int
                                     int32_t d_cb, int32_t d_r, int32_t page_size, int32_t max_seq_len, int32_t dtype,
                                     int32_t* info);
 
+/* The same for mlra_mx4_decode_attn (arguments as there; with_lse: 1 if lse is given), on tensors that start at multiples of 16
+ * bytes.  info is a HOST array of 7 values:
+ *   [0] decode kernel, on the codes as they are cached: 1 MFMA plain form, 2 MFMA PAIRED form, 4 MFMA MLA kernel; 6 the kernel
+ *       for every shape, which widens them first
+ *   [1] chunk slots per (query token, block)   [2] uniform chunk length in tokens
+ *   [3] > 0: the decode kernel fits the chunk length to the lengths, at least this one (see mlra_decode_route_info)
+ *   [4] 1: a planning kernel cuts the chunks   [5] 1: the epilogue is the bf16 one, 0: the fp32 one
+ *   [6] 1: bf16 operands, and an fp32 out or a log-sum-exp exact to fp32 */
+MLRA_API int mlra_mx4_decode_plan_info(int32_t batch, int32_t q_len, int32_t h, int32_t d_h, int32_t groups, int32_t n_blocks,
+                                       int32_t d_cb, int32_t d_r, int32_t page_size, int32_t max_pages_per_seq,
+                                       int32_t dtype, int32_t out_dtype, int32_t with_lse, int32_t* info);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,7 @@ EXPORTS = ("mlra_strerror", "mlra_append_kv", "mlra_absorb_q", "mlra_absorb_q_fo
            "mlra_mx4_append_kv", "mlra_mx4_read_kv", "mlra_mx4_decode_workspace_bytes", "mlra_mx4_decode_attn",
            "mlra_mx4_pre_attention_workspace_bytes", "mlra_mx4_pre_attention",
            "gqa_decode_workspace_bytes", "gqa_decode_attn", "mlra_kernel_timing_begin",
-           "mlra_kernel_timing_end", "mlra_decode_plan_info", "mlra_decode_route_info", "mlra_probe_stream_read", "mlra_probe_shader_clock")
+           "mlra_kernel_timing_end", "mlra_decode_plan_info", "mlra_decode_route_info", "mlra_mx4_decode_plan_info", "mlra_probe_stream_read", "mlra_probe_shader_clock")
 
 
 class _CacheStruct(ctypes.Structure):
@@ -120,6 +120,8 @@ def load_library() -> ctypes.CDLL:
     lib.mlra_decode_plan_info.argtypes = [i32] * 10 + [ctypes.POINTER(ctypes.c_int32)]
     lib.mlra_decode_route_info.restype = ctypes.c_int
     lib.mlra_decode_route_info.argtypes = [i32] * 11 + [ctypes.POINTER(ctypes.c_int32)]
+    lib.mlra_mx4_decode_plan_info.restype = ctypes.c_int
+    lib.mlra_mx4_decode_plan_info.argtypes = [i32] * 13 + [ctypes.POINTER(ctypes.c_int32)]
     lib.gqa_decode_workspace_bytes.restype = sz
     lib.gqa_decode_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.gqa_decode_attn.restype = ctypes.c_int
@@ -618,7 +620,7 @@ def gqa_decode_attn(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torc
     return out
 
 
-DECODE_KERNELS = ("generic", "mfma", "mfma-paired", "mfma-gla", "mfma-mla", "f32")
+DECODE_KERNELS = ("generic", "mfma", "mfma-paired", "mfma-gla", "mfma-mla", "f32", "mx4")
 
 
 def mlra_decode_plan_info(batch: int, h: int, d_h: int, groups: int, n_blocks: int, d_cb: int, d_r: int,
@@ -639,6 +641,17 @@ def mlra_decode_route_info(batch: int, h: int, d_h: int, groups: int, n_blocks: 
                                                  _dt(dtype), info), "mlra_decode_route_info")
     return {"chunk_slots": info[0], "fitted_from": info[1], "planned": bool(info[2]),
             "mla_stages": None if info[3] < 0 else info[3]}
+
+
+def mlra_mx4_decode_plan_info(batch: int, h: int, d_h: int, groups: int, n_blocks: int, d_cb: int, d_r: int, page_size: int,
+                              max_pages_per_seq: int, dtype: torch.dtype, out_dtype: torch.dtype, with_lse: bool = False,
+                              q_len: int = 1) -> dict:
+    """Which kernels and which context split a decode call on a cache in 4 bits takes (host logic only)."""
+    info = (ctypes.c_int32 * 7)()
+    _check(load_library().mlra_mx4_decode_plan_info(batch, q_len, h, d_h, groups, n_blocks, d_cb, d_r, page_size, max_pages_per_seq,
+                                                    _dt(dtype), _dt(out_dtype), int(with_lse), info), "mlra_mx4_decode_plan_info")
+    return {"kernel": DECODE_KERNELS[info[0]], "chunk_slots": info[1], "chunk_tokens": info[2], "fitted_from": info[3],
+            "planned": bool(info[4]), "merge_mfma": bool(info[5]), "precise": bool(info[6])}
 
 
 def mlra_kernel_timing_begin(max_calls: int) -> None:

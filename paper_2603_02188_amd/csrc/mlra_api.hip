@@ -143,7 +143,7 @@ static void carve_workspace(DecodeArgs& a, void* workspace) {
   a.unit_tab = (int32_t*)((char*)a.chunk_tab + align_up((size_t)a.batch * sizeof(int32_t), 256));
 }
 
-// (mlra_decode_plan_info [0]; 2: kMlra, paired.  kMx4: the kernel for every shape of a cache in 4 bits)
+// (mlra_decode_plan_info [0], mlra_mx4_decode_plan_info [0]; 2: kMlra, paired.  kMx4: the kernel for every shape of a cache in 4 bits)
 enum DecodeKernel { kPlain = 0, kMlra = 1, kGla = 3, kMla = 4, kF32 = 5, kMx4 = 6 };
 struct Route {
   DecodeKernel kernel;
@@ -329,6 +329,14 @@ static SplitPlan plan_mx4_fast(int units, int q_len, int h, int groups, int n_bl
   return two;
 }
 
+// a.precise and a.plan of a call on a cache in 4 bits, whose shape, types and addresses are set
+static void plan_mx4_decode(DecodeArgs& a) {
+  const int max_seq_len = a.max_pages * a.page_size;
+  a.precise = a.dtype == MLRA_BF16 && (a.out_dtype == MLRA_F32 || a.lse);
+  a.plan = plan_mx4_fast(a.batch, a.q_group, a.h, a.groups, a.n_blocks, a.d_cb, max_seq_len, a.cus);
+  if (!mx4_pipelined(a)) a.plan = plan_mx4(a.batch, a.h, a.n_blocks, a.d_cb, a.dtype, max_seq_len, a.cus);
+}
+
 // (q_len > 1: a row of the lengths and of the page table per query in front of the partials)
 static size_t mx4_table_bytes(int units, int q_len, int max_pages) {
   return q_len == 1 ? 0 : align_up((size_t)units * sizeof(int32_t), 256) +
@@ -428,13 +436,12 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   if (d_h <= 0 || c->d_r > kMx4MaxRope ||
       !mx4_shape_ok(batch, q_len, h, groups, c->n_blocks, c->d_cb, c->page_size, c->max_pages_per_seq))
     return MLRA_ERR_SHAPE;
-  const int units = batch * q_len, hb = h / groups, max_seq_len = c->max_pages_per_seq * c->page_size;
+  const int units = batch * q_len, hb = h / groups;
   const size_t need = mlra_mx4_decode_workspace_bytes(batch, q_len, h, groups, c->n_blocks, c->d_cb, c->page_size,
                                                       c->max_pages_per_seq);
   if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 256 != 0) return MLRA_ERR_WORKSPACE;
   DecodeArgs a = {};
   a.cus = device_cu_count();
-  a.plan = plan_mx4_fast(units, q_len, hb, groups, c->n_blocks, c->d_cb, max_seq_len, a.cus);
   a.latent = c->latent;
   a.scales = c->scales;
   a.rope = c->rope;
@@ -463,8 +470,7 @@ int mlra_mx4_decode_attn(const mlra_mx4_cache* c, int32_t batch, int32_t q_len, 
   a.stream = (hipStream_t)stream;
   a.t_main = timing_pair(0);
   a.t_epi = timing_pair(1);
-  a.precise = c->dtype == MLRA_BF16 && (out_dtype == MLRA_F32 || lse);
-  if (!mx4_pipelined(a)) a.plan = plan_mx4(units, hb, c->n_blocks, c->d_cb, c->dtype, max_seq_len, a.cus);
+  plan_mx4_decode(a);
   int32_t* const lens = (int32_t*)workspace;
   int32_t* const table = (int32_t*)((char*)workspace + align_up((size_t)units * sizeof(int32_t), 256));
   carve_workspace(a, (char*)workspace + mx4_table_bytes(units, q_len, c->max_pages_per_seq));
@@ -737,6 +743,43 @@ int mlra_decode_route_info(int32_t batch, int32_t q_len, int32_t h, int32_t d_h,
   info[1] = a.fitted ? a.fit_tiles * 64 : 0;
   info[2] = r.planned ? 1 : 0;
   info[3] = r.kernel == kMla ? mla_mfma_stages(a) : -1;
+  return MLRA_OK;
+}
+
+int mlra_mx4_decode_plan_info(int32_t batch, int32_t q_len, int32_t h, int32_t d_h, int32_t groups, int32_t n_blocks,
+                              int32_t d_cb, int32_t d_r, int32_t page_size, int32_t max_pages_per_seq, int32_t dtype,
+                              int32_t out_dtype, int32_t with_lse, int32_t* info) {
+  if (!info) return MLRA_ERR_NULL;
+  if (!valid_dtype(dtype) || !valid_dtype(out_dtype)) return MLRA_ERR_DTYPE;
+  if (d_h <= 0 || d_r <= 0 || d_r > kMx4MaxRope ||
+      !mx4_shape_ok(batch, q_len, h, groups, n_blocks, d_cb, page_size, max_pages_per_seq))
+    return MLRA_ERR_SHAPE;
+  float there = 0.f;         // (an address: the route asks whether there is a log-sum-exp, and scales)
+  DecodeArgs a = {};
+  a.cus = device_cu_count();
+  a.scales = (const void*)256;
+  a.page_size = page_size;
+  a.max_pages = max_pages_per_seq;
+  a.n_blocks = n_blocks;
+  a.d_cb = d_cb;
+  a.d_r = d_r;
+  a.batch = batch * q_len;
+  a.h = h / groups;
+  a.d_h = d_h;
+  a.groups = groups;
+  a.out_dtype = out_dtype;
+  a.lse = with_lse ? &there : nullptr;
+  a.q_group = q_len;
+  a.dtype = dtype;
+  plan_mx4_decode(a);
+  const Route r = choose_route(a);
+  info[0] = r.kernel == kMlra && decode_mfma_paired(a.h, n_blocks, groups) ? 2 : (int)r.kernel;
+  info[1] = a.plan.n_splits;
+  info[2] = a.plan.chunk_tokens;
+  info[3] = a.fitted ? a.fit_tiles * 64 : 0;
+  info[4] = r.planned ? 1 : 0;
+  info[5] = r.merge_mfma ? 1 : 0;
+  info[6] = a.precise ? 1 : 0;
   return MLRA_OK;
 }
 
