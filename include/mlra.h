@@ -122,7 +122,7 @@ MLRA_API size_t mlra_decode_workspace_bytes(int32_t batch, int32_t h, int32_t n_
  *              (they then carry tau log2(e) and the scores are not scaled again).
  * A NaN or an infinity in a query or a row reaches its own sequence only, and in a query its own head, but for bf16 caches with
  * blocks of 128 or 256 channels and d_r = 64: there the row sums of heads i and i + 16 (i / 16 even) come from one matrix
- * product, and a NaN of one makes NaN of both.
+ * product, and a NaN of one makes NaN of both, as a score of -inf (an infinite key) in a chunk's last tile of 64 tokens may.
  * Context is split into chunks processed by independent workgroups whose partial (max, sum, z) are
  * merged with a log-sum-exp merge; results are deterministic (no atomics). */
 MLRA_API int mlra_decode_attn(const mlra_cache* cache, int32_t batch, int32_t h, int32_t d_h, const void* q_abs,

@@ -829,6 +829,10 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
     }
     float mx0, mx1;
     col_max2(sa0, sa1, mx0, mx1);
+    if (MX4) {       // (scores of -inf, from infinite keys, are no reference)
+      mx0 = mx0 > -INFINITY ? mx0 : 0.f;
+      mx1 = mx1 > -INFINITY ? mx1 : 0.f;
+    }
     m_run[0] = mx0;
     m_run[1] = mx1;
 #pragma unroll
@@ -1125,6 +1129,10 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
       l_run[nt] = l_sum[nt] + __shfl_xor(l_sum[nt], 32);
       m_run[nt] *= sc;
     }
+  }
+  if (MX4) {         // (a wave without weight does not set the scale)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) m_run[nt] = l_run[nt] == 0.f ? -3.0e38f : m_run[nt];
   }
   if (MX4) {      // (the last step has widened a tile into the ring, which nothing reads: it lands before the ring is reused)
     wait_vm_lgkm<63>();

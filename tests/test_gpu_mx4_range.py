@@ -85,6 +85,28 @@ def test_queries_that_are_not_finite_reach_their_heads_only(n_blocks, d_cb, h, g
             assert torch.equal(lse[1][:, 0][same], lse[0][:, 0][same]) and not lse[1][:, 0][~same].isfinite().any()
 
 
+@pytest.mark.parametrize("with_lse", [False, True])
+@pytest.mark.parametrize("n_blocks,d_cb,h", SHAPES + [(3, 128, 100)])
+def test_keys_of_minus_infinity_in_bf16(n_blocks, d_cb, h, with_lse):
+    """Tokens whose score is -inf for every head, which have no weight: one among others, a tile, the last token, alone in its tile,
+    and all of a chunk's but the first ones."""
+    lens, tau = [500, 65, 129, 1200], 1.0 / np.sqrt(192)
+    hc = HostCache(lens, n_blocks, d_cb, 64, "bf16", 64, 81)
+    for s, tokens in enumerate(([7, 499], [64], list(range(64, 129)), list(range(70, 1200)))):
+        for t in tokens:
+            hc.rope[hc.table[s, t // 64], t % 64, 5] = hc.ropes[s][t, 5] = -np.inf
+    rng = np.random.default_rng(82)
+    (qa, qa64), (_, qr64), (wv, wv64) = queries(rng, 4, 1, n_blocks, h, 1, d_cb, 64, 128, "bf16")
+    qr64[..., 5] = np.abs(qr64[..., 5]) + 0.1
+    qr, qr64 = stored(qr64, "bf16")
+    lse = torch.empty((4, 1, n_blocks, h), device="cuda") if with_lse else None
+    got = mlra.mlra_mx4_decode_attn(hc.device(), qa, qr, wv, tau, lse=lse).double().cpu().numpy()
+    ref, ref_lse = orc.attend(hc.rows, hc.ropes, lens, qa64, qr64, wv64, tau)
+    assert max_rel_err(got, ref) <= BF16_BAR
+    if with_lse:
+        assert np.abs(lse.double().cpu().numpy() - ref_lse).max() <= 1e-2         # (exact to fp32: see the other tests' bars)
+
+
 # fp32: RoPE numbers are the sum of three of bf16 there, whose products with an infinite one are NaN or infinities of either sign
 F32 = [(4, 128, 64, 128), (2, 64, 32, 40), (1, 512, 64, 20), (2, 256, 128, 16), (2, 128, 128, 8)]
 
