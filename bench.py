@@ -87,7 +87,7 @@ def _cpu_baseline(inp, max_seconds=25.0):
                       f"{dt:.1f} s of fp64 numpy, scaled to the whole batch by token count"}, np.stack(outs)
 
 
-_DECODE_KERNEL_SOURCES = ("decode_mfma.hip", "chunk_fit.h", "mfma_tile.h", "proj_mfma.hip")
+_DECODE_KERNEL_SOURCES = ("decode_mfma.hip", "decode_mfma_kernel.h", "chunk_fit.h", "mfma_tile.h", "proj_mfma.hip")
 
 
 def _kernel_sources_digest():
