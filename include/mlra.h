@@ -311,14 +311,15 @@ MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, in
  * The arithmetic of a bf16 call with a bf16 output is that of a cache of type dtype that holds the same values: queries (with
  * the softmax scale), probabilities and merged values are rounded to bf16, or the queries of a group of 32 channels to 2^-8 of
  * its largest (2^-13 where that stands out), 0.11 % in the mean.  fp32 rounds nothing to fewer than 24 bits, and neither do an
- * fp32 out of a bf16 call (out_dtype MLRA_F32) and the lse beside it, by a kernel that takes about twice the time.  Beside a bf16
- * out, lse is exact to fp32 but for query channels below 2^-6 of their group's largest, which are rounded to 2^-15 of that (blocks
- * of 128 channels and MLA; others take the slower kernel).
+ * fp32 out of a bf16 call (out_dtype MLRA_F32) and the lse beside it, by a kernel that takes two and a half to three times as long.
+ * Beside a bf16 out, lse is exact to fp32 but for query channels below 2^-6 of their group's largest, which are rounded to 2^-15 of
+ * that (blocks of 128 channels and MLA, a tenth longer than without lse; others take the slower kernel).  Asking for it changes the
+ * arithmetic, and so out within its rounding: to the last bit it is the same from call to call, not with lse and without.
  * A query without a row gives zeros and lse = -inf.  A NaN or an infinity in a query makes NaN of its own head's output (by the
- * formula it does).  A score that overflows fp32 although query and row are finite, or that an infinite RoPE key makes infinite, can
- * make NaN of the head 16 away as well beside a bf16 out without lse (see mlra_decode_attn).  Scales, queries and weights may start at any multiple of their element's
- * size; at multiples of 16 bytes the faster kernels take them.  d_cb <= 512, d_r <= 128; preconditions on pages and lengths as
- * for mlra_decode_attn.  Deterministic. */
+ * formula it does).  A score that overflows fp32 although query and row are finite, or that an infinite RoPE key makes infinite,
+ * can make NaN of the head 16 away as well beside a bf16 out without lse (see mlra_decode_attn).
+ * Scales, queries and weights may start at any multiple of their element's size; at multiples of 16 bytes the faster kernels take
+ * them.  d_cb <= 512, d_r <= 128; preconditions on pages and lengths as for mlra_decode_attn.  Deterministic. */
 MLRA_API int mlra_mx4_decode_attn(const mlra_mx4_cache* cache, int32_t batch, int32_t q_len, int32_t h, int32_t d_h,
                          int32_t groups, const void* q_abs, const void* q_rope, const void* w_uv, const void* gate,
                          float softmax_scale, float out_scale, void* out, int32_t out_dtype, float* lse, void* workspace,

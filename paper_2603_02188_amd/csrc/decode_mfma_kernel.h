@@ -39,10 +39,10 @@
 // wrong axis for that instruction (a scale per token, which is the k index there), two tiles are widened to bf16, which is
 // exact: each wave widens the 16 rows that it loaded itself, tile j + 2 behind the value MFMAs of step j, into the place of
 // tile j.  64 sequences of 8192 tokens, 128 heads, four blocks: 137 us, 1.25 PFLOP/s of the model's operations (172 us with the
-// scores in bf16); the matrix pipe is busy for 56 % of it.
+// scores in bf16); the matrix pipe is busy for 55 % of it.
 // EXACT, for a log-sum-exp beside a bf16 output: queries as they are, in three rows, the softmax scale in front of exp2 and row
-// sums on the vector pipe, of probabilities that are not rounded.  128 sequences of 512 to 8192 tokens, whole steps: 187 us, 172
-// without the log-sum-exp, 436 on the kernel for every shape.
+// sums on the vector pipe, of probabilities that are not rounded.  128 sequences of 512 to 8192 tokens, gated, whole steps: 196 us,
+// 181 without the log-sum-exp (436 and 396 on the kernel for every shape).
 #pragma once
 
 #include "chunk_fit.h"
@@ -640,7 +640,8 @@ __global__ __launch_bounds__(256) void decode_mfma_kernel(MfmaParams p) {
   auto score_first = [&](f32x16& acc, const bf16x8& kt, const bf16x8& qt, const f32x16& init) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(acc) : "v"(kt), "a"(qt), "v"(init));
   };
-  // (MX4) S^T += K Q^T for 64 channels: E2M1 codes with their scales against one of the two E2M3 terms of a query
+  // (MX4) S^T += K Q^T for 64 channels: E2M1 codes with their scales against one E2M3 term of a query, whose scale is byte
+  // 2 ks + term of qsc (the third terms' are in a register of their own, as the first of two)
   auto score_mx = [&](f32x16& acc, int ks, int term, const u32x6& qt, unsigned qsc) {
     switch (2 * ks + term) {
       case 0: asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:2"

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void gqa_mfma_kernel(GqaMfmaParams p) {
     }
   };
 
-  // per-lane LDS read offsets inside a stage (see decode_mfma.hip)
+  // per-lane LDS read offsets inside a stage (see decode_mfma_kernel.h)
   const unsigned k_off = c32 * (kGDh * 2) + ((g ^ lat_swz(c32)) << 4);           // ^ (ks << 5)
   unsigned v_off[2];                                                            // ^ (mt << 6), + 4096 ss
   {

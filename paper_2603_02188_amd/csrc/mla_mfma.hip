@@ -222,7 +222,7 @@ __global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void mla_mfma_kernel(Mfma
     }
   };
 
-  // ---- per-lane LDS read offsets inside a stage (XOR swizzle, see mfma_tile.h and decode_mfma.hip).
+  // ---- per-lane LDS read offsets inside a stage (XOR swizzle, see mfma_tile.h and decode_mfma_kernel.h).
   // Scores, A operand of the 16x16x32 MFMA: lane = operand row c16 (+ 16 th) and eight channels from
   // 32 ks + 8 q4, i.e. 16-byte chunk 4 ks + q4 of the token row: sub-row ks / 4, chunk 4 (ks % 4) + q4.
   // A 128-bit LDS read is served sixteen lanes a cycle, and the sixteen are lanes 0-3, 12-15, 20-27 (then
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void mla_mfma_kernel(Mfma
       __builtin_amdgcn_sched_barrier(0);
     }
 
-    // ---- softmax of the 16 heads (running maximum refreshed lazily, see decode_mfma.hip)
+    // ---- softmax of the 16 heads (running maximum refreshed lazily, see decode_mfma_kernel.h)
     float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     mx = head_max(mx);
@@ -440,8 +440,8 @@ constexpr int kXThirdBytes = 8 * 64 * 24, kXLds = kXThird + 2 * kXThirdBytes;
 static_assert(kXLds <= 160 * 1024, "one workgroup per CU");
 
 // EXACT (4 bits, a log-sum-exp exact to fp32 is wanted): all queries as three numbers.  (The softmax scale is behind the scores
-// and the row sums are of unrounded probabilities in any case.)  64 sequences of 512 to 4096 tokens, whole steps: 119 us, 103
-// without the log-sum-exp, 313 with an fp32 output, on the kernel for every shape.
+// and the row sums are of unrounded probabilities in any case.)  64 sequences of 512 to 4096 tokens, whole steps: 110 us, 99
+// without the log-sum-exp (252 on the kernel for every shape), 306 with an fp32 output, on that kernel.
 template <bool MX4, bool EXACT = false>
 __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
   constexpr int kStageB = MX4 ? kXStage : kMStage, kRopeOff = MX4 ? kXRope : kMLatBytes;
@@ -755,7 +755,7 @@ __global__ __launch_bounds__(256, 1) void mla_pipe_kernel(MfmaParams p) {
     mx = fmaxf(a, b);
     ((float*)(smem + kPX))[(par * 4 + wave) * 32 + c32] = mx;
   };
-  // The reference maxima (refreshed lazily, see decode_mfma.hip) from both halves' maxima; when one moves, its factor is
+  // The reference maxima (refreshed lazily, see decode_mfma_kernel.h) from both halves' maxima; when one moves, its factor is
   // left for the waves that hold the head's history (both halves store the same).
   auto refresh = [&](float partner, int par, int tile) {
     const float cand = fmaxf(mx, partner) * sc;
