@@ -315,8 +315,8 @@ MLRA_API size_t mlra_mx4_decode_workspace_bytes(int32_t batch, int32_t q_len, in
  * Beside a bf16 out, lse is exact to fp32 but for query channels below 2^-6 of their group's largest, which are rounded to 2^-15 of
  * that (blocks of 128 channels and MLA, a tenth longer than without lse; others take the slower kernel).  Asking for it changes the
  * arithmetic, and so out within its rounding: to the last bit it is the same from call to call, not with lse and without.
- * A query without a row gives zeros and lse = -inf.  A NaN or an infinity in a query makes NaN of its own head's output (by the
- * formula it does).  A score that overflows fp32 although query and row are finite, or that an infinite RoPE key makes infinite,
+ * A query without a row gives zeros and lse = -inf, and so may one all of whose scores are -inf.  Otherwise a NaN or an infinity in
+ * a query makes NaN of its own head's output, as by the formula.  A score that overflows fp32 although query and row are finite, or that an infinite RoPE key makes infinite,
  * can make NaN of the head 16 away as well beside a bf16 out without lse (see mlra_decode_attn).
  * Scales, queries and weights may start at any multiple of their element's size; at multiples of 16 bytes the faster kernels take
  * them.  d_cb <= 512, d_r <= 128; preconditions on pages and lengths as for mlra_decode_attn.  Deterministic. */

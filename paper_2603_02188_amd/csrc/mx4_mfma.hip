@@ -18,7 +18,8 @@
 //   * rows are 16 bytes longer than their channels, so that sixteen rows start in sixteen different bank groups.
 //   * forms: block width and RoPE width as the tile is padded to (64 to 512, 64 and 128), 32 or 64 heads (mx4_heads_per_wg), terms of a
 //     probability, and VEC = false for RoPE widths that are no multiple of four and for tensors that start in between.
-//     Registers: none is spilled but in fp32 with 512 and 128 channels, on the way that computes scores again.
+//     Registers are spilled in fp32 with 512 and 128 channels only: four in front of the loop, others on the way that computes
+//     scores again.
 // Bound by the vector instructions of a tile (widening, splitting, softmax: 600 to 700 a wave) and their latency.  fp32, 8
 // sequences of 300 to 2048 tokens, 128 heads, four blocks: 32 us, and 17 for the merge; bf16 with an fp32 output, 16 sequences of
 // 1000 to 4093, four query tokens: 155 us, and 51 for the merge.
