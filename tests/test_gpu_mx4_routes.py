@@ -89,3 +89,44 @@ def test_query_channels_that_hardly_stand_out(n_blocks, d_cb, h, groups):
     err = max_rel_err(got, ref)
     print(f"       max rel err {err:.3e}, scores off by {off:.2e}", flush=True)
     assert err <= 1e-2 + 2.0 ** -8 + 5.0 * off / 3.5
+
+
+@pytest.mark.parametrize("kw", [dict(n_blocks=4, d_cb=128, h=128, batch=8, pages=512), dict(n_blocks=1, d_cb=512, h=128, batch=20, pages=256),
+                                dict(n_blocks=4, d_cb=128, h=128, batch=5, pages=256, q_len=3), dict(n_blocks=4, d_cb=128, h=64, batch=100, pages=32)])
+@pytest.mark.parametrize("with_lse", [False, True])
+def test_captured_calls_with_other_lengths(kw, with_lse):
+    """A decode call in a HIP graph, whose chunks follow the lengths on the device: replays with other lengths (longer and shorter than
+    at the capture, zero among them) equal the eager call, with eager work in between."""
+    n_blocks, d_cb, h, batch, pages, q_len = (kw.get(k, 1) for k in ("n_blocks", "d_cb", "h", "batch", "pages", "q_len"))
+    info = mlra.mlra_mx4_decode_plan_info(batch, h, 128, 1, n_blocks, d_cb, 64, 64, pages, torch.bfloat16, torch.bfloat16, with_lse, q_len)
+    assert info["kernel"] != "mx4" and (info["fitted_from"] > 0) == (batch <= 64)
+    rng = np.random.default_rng(91)
+    (qa, _), (qr, _), (wv, _) = queries(rng, batch, q_len, n_blocks, h, 1, d_cb, 64, 128, "bf16")
+    g = torch.Generator("cuda").manual_seed(92)
+    table = torch.randint(0, 64, (batch, pages), generator=g, device="cuda", dtype=torch.int32)       # (shared pages)
+    lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    cache = mlra.Mx4Cache.empty(64, n_blocks, 64, d_cb, 64, table, lens)
+    cache.latent.random_(0, 256, generator=g)
+    cache.scales.random_(123, 129, generator=g)
+    cache.rope.normal_(generator=g)
+    ws = torch.empty(mlra.mlra_mx4_decode_workspace_bytes(batch, q_len, h, 1, n_blocks, d_cb, 64, pages), dtype=torch.uint8, device="cuda")
+    out = torch.empty((batch, q_len, h, 128), dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty((batch, q_len, n_blocks, h), device="cuda") if with_lse else None
+    call = lambda o, l, w: mlra.mlra_mx4_decode_attn(cache, qa, qr, wv, 0.07, out=o, lse=l, workspace=w)
+    lens.fill_(1000)
+    call(out, lse, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, lse, ws)
+    for i, most in enumerate((64 * pages, 100, 5000, 64 * pages, 1)):
+        lens.copy_(torch.from_numpy(rng.integers(0, min(most, 64 * pages) + 1, batch).astype(np.int32)))
+        lens[i % batch] = min(most, 64 * pages)
+        want_lse = torch.empty_like(lse) if with_lse else None
+        want = call(torch.empty_like(out), want_lse, torch.empty_like(ws))
+        out.fill_(9.0)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and out.isfinite().all() and (not with_lse or torch.equal(lse, want_lse)), i
